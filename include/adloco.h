@@ -59,13 +59,15 @@ extern "C" {
 #define ADLOCO_F16   2   /* IEEE half: the mixed-precision setting of the paper's experiments (Section 6) */
 
 /* ---- flags -------------------------------------------------------------------------- */
-#define ADLOCO_ACCUMULATE       0x1u  /* grad_stats: continue a batch (switch mode micro-batch) */
+#define ADLOCO_ACCUMULATE       0x1u  /* grad_stats: continue a batch (switch mode micro-batch);
+                                         block_product: add to the output                        */
 #define ADLOCO_SUM_ONLY         0x2u  /* grad_stats: form the gradient sums only, no norms       */
 #define ADLOCO_GRAD_PROVIDED    0x1u  /* linear_desc.flags: caller maintains grad_sum itself     */
 /* linear_desc.flags, bits 4..7: which block of the parameters the descriptor stands for      */
 #define ADLOCO_KIND_LINEAR      0x00u /* weight W [d_out, d_in] of a linear layer (the default)  */
 #define ADLOCO_KIND_VECTOR      0x10u /* vector p [d_out] used element-wise: a bias or a gain    */
 #define ADLOCO_KIND_EMBED       0x20u /* embedding table E [d_in, d_out], a = int32 token ids    */
+#define ADLOCO_KIND_SAMPLE_SUMS 0x30u /* vector p [d_out] whose per-sample gradients are at hand   */
 #define ADLOCO_KIND_MASK        0xf0u
 #define ADLOCO_BROADCAST        0x1u  /* outer_step: also write the new outer model into theta_k */
 #define ADLOCO_BIASED_VAR       0x1u  /* norm_test: variance normalised by 1/B instead of 1/(B-1)*/
@@ -117,7 +119,10 @@ typedef struct {
  *     tokens with id v, so ||g_i||^2 = sum_{t,t'} [id_t = id_t'] delta_t . delta_t'.  The table
  *     gradient itself is the caller's: ADLOCO_GRAD_PROVIDED is required, grad_sum [V, d_out] is
  *     only read (by adloco_norm_test) and may be NULL in adloco_grad_stats.  T <= 8192.
- * Both kinds stream delta (and x) once; their sums run in a fixed order.  A gain and a bias that are
+ * ADLOCO_KIND_SAMPLE_SUMS  a vector p [d_out] whose per-sample gradients are formed already (by
+ *     adloco_rms_norm_backward): `delta` = fp32 [B, d_out] whatever `dtype` is, samples delta_row_stride
+ *     apart, 4-byte aligned; `a` must be NULL, d_in 1; grad_sum is [d_out].
+ * The first two kinds stream delta (and x) once; their sums run in a fixed order.  A gain and a bias that are
  * given the same delta tensor (the two vectors of a normalisation layer) are formed in one pass
  * over it.  All kernels run on `stream`, one after the other. */
 
@@ -453,6 +458,112 @@ typedef struct {
 int adloco_round(adloco_ctx* ctx, const adloco_round_config* cfg, adloco_trainer* trainers, int* k,
                  const adloco_linear_desc* layers, int n_layers, size_t N, adloco_batch_fn batch_fn,
                  adloco_round_report* reports, void* stream);
+
+/* ------------------------------------------------------------------------------------ *
+ * Layer operators: the arithmetic of a transformer layer around the blocks whose gradients are
+ * measured above, as a worker's forward and backward pass (the caller's, `batch_fn` of adloco_round)
+ * needs it.  A sublayer's way: h = residual + dropout(x), y = rms_norm(h) in 16 bits (the activations
+ * that adloco_grad_stats reads) and in 8-bit blocks; the layer's output, its input gradient and its
+ * gradient sum (ADLOCO_GRAD_PROVIDED) as products of 8-bit blocks; the norm's backward pass, whose
+ * gain_sums are an ADLOCO_KIND_SAMPLE_SUMS block of the statistics.
+ * Matrices are rows of d contiguous values of `dtype` (ADLOCO_F32, ADLOCO_BF16, ADLOCO_F16), a row
+ * stride apart (elements; 0: d), aligned to their element size.  Rows that are 16-byte aligned with
+ * d % 8 == 0 take the vector path, others a guarded one with the same results.  An output may be the
+ * very rows of an input (same address and stride) where that is said below, and must not overlap
+ * anything else.  Arithmetic is fp32 in registers, each output rounded once.  No rows are a
+ * successful no-op.  The context's device is made current for the call.
+ * All of these calls can be captured.  adloco_rms_norm_backward (with gain_sums) and
+ * adloco_block_product split long sums over the chip when the first eager call that does so could
+ * take 64 MiB of scratch memory for the context, which then stays where it is; a captured call that
+ * finds none takes each sum in one piece (same results up to fp32 summation order, slower).
+ *
+ * Dropout.  The mask is never stored: Philox4x32-10 with the key `seed` (low word, high word) and the
+ * counter (column / 8, row, row >> 32, 0) gives 16-bit numbers for the eight columns (word i: low half
+ * to column 2 i, high half to 2 i + 1), and the element is dropped where its number is below t =
+ * round(65536 p); the others are scaled by 65536 / (65536 - t).  row = first_row + the row of the call:
+ * a batch that SwitchMode cuts into micro-batches keeps its masks if first_row counts on.  Dropped
+ * values become 0 whatever they are.  The backward pass is the same call on the gradient.
+ * ------------------------------------------------------------------------------------ */
+typedef struct {
+  double   p;                   /* share to drop, in [0, 1); steps of 2^-16                          */
+  uint64_t seed;
+  int64_t  first_row;           /* >= 0                                                              */
+} adloco_dropout_mask;
+
+/* adloco_dropout: out = residual + dropout(x), or out = dropout(x) with residual NULL.  out may be x or
+ * residual.  At most 2^31 - 1 groups of 64 x 8 columns. */
+int adloco_dropout(adloco_ctx* ctx, const void* x, int64_t x_row_stride, const void* residual,
+                   int64_t residual_row_stride, void* out, int64_t out_row_stride, int64_t rows, int32_t d,
+                   int dtype, const adloco_dropout_mask* mask, void* stream);
+
+/* A matrix in 8-bit blocks, device memory of the caller: 128 consecutive values of a row share a power
+ * of two.  Value (r, c) is data[r * row_stride + c] (e4m3: 4 exponent bits, 3 mantissa bits, largest
+ * 448, no infinity) times 2^(exponent[(c / 128) * exponent_stride + r] - 127).  Rows hold whole blocks:
+ * the bytes from cols up to the next multiple of 128 are zero (the calls that write blocks see to it, and
+ * adloco_block_product relies on it).  A block's exponent is the smallest, from 1 on, with which its largest
+ * finite value fits; values are rounded to nearest even (at most 2^-4 of a value, and 2^-10 of the
+ * power of two below 2^-6 of it); infinities and NaN become NaN. */
+typedef struct {
+  void*    data;                /* 16-byte aligned                                                   */
+  uint8_t* exponent;            /* [ceil(cols / 128), exponent_stride], 16-byte aligned              */
+  int64_t  rows, cols;          /* cols >= 1                                                         */
+  int64_t  row_stride;          /* bytes, >= cols up to a multiple of 128; a multiple of 16          */
+  int64_t  exponent_stride;     /* bytes, >= rows; a multiple of 16                                  */
+} adloco_blocks8;
+
+/* adloco_pack_blocks: a matrix [rows, cols] to blocks along its rows (along: rows x cols) and / or across
+ * them (across: the transpose, cols x rows); either may be NULL.  x is read once for both. */
+int adloco_pack_blocks(adloco_ctx* ctx, const void* x, int64_t x_row_stride, int64_t rows, int64_t cols,
+                       int dtype, const adloco_blocks8* along, const adloco_blocks8* across, void* stream);
+
+/* adloco_block_product: out [a.rows, b.rows] = a b^T, both operands along the axis that is summed over
+ * (a.cols == b.cols).  With activations x8 [T, d_in] and W8 [d_out, d_in] the layer's output; with
+ * delta8 [T, d_out] and W packed across [d_in, d_out] the input gradient; with delta and x packed across
+ * ([d_out, T] and [d_in, T]) the gradient sum, fp32, with ADLOCO_ACCUMULATE added to what is there.
+ * Products are exact, sums fp32, one rounding at the end; only an fp32 output accumulates.  A NaN in
+ * row m of a makes row m of out NaN, one in row n of b column n. */
+int adloco_block_product(adloco_ctx* ctx, const adloco_blocks8* a, const adloco_blocks8* b, void* out,
+                         int64_t out_row_stride, int dtype, uint32_t flags, void* stream);
+
+/* adloco_rms_norm: h = residual + dropout(x);  y = h / sqrt(mean(h^2) + eps) * gain.  The mean is of h in
+ * fp32, before it is rounded to `dtype`.
+ *   x, h, y     [rows, d]; h and y may each be x or residual, and NULL if not wanted
+ *   residual    [rows, d] or NULL (h = dropout(x))
+ *   gain        device [d] fp32, or NULL for ones
+ *   mask        NULL or p = 0: no dropout
+ *   y8          y in 8-bit blocks (rounded from fp32), or NULL; at least one of h, y, y8
+ * d <= 16384; eps a positive normal fp32 number. */
+typedef struct {
+  const void*  x;
+  const void*  residual;
+  const float* gain;
+  void*        h;
+  void*        y;
+  int64_t x_row_stride, residual_row_stride, h_row_stride, y_row_stride;
+} adloco_norm_io;
+int adloco_rms_norm(adloco_ctx* ctx, const adloco_norm_io* io, int64_t rows, int32_t d, int dtype, double eps,
+                    const adloco_dropout_mask* mask, const adloco_blocks8* y8, void* stream);
+
+/* adloco_rms_norm_backward: from h as stored and the gradient dy of y, with n = h / sqrt(mean(h^2) + eps):
+ *   dh = dh_in + (gain dy - n mean(gain dy n)) / sqrt(mean(h^2) + eps)
+ *   dx = dropout(dh) with the mask of the forward call (NULL or p = 0: dx = dh)
+ *   gain_sums[i] = sum over the T rows of sample i of dy n
+ *   h, dy, dh, dx  [B * T, d]; dh and dx may each be h, dy or dh_in; at least one of dh, dx, gain_sums
+ *   dh_in          [B * T, d] or NULL: the gradient that reaches h on the residual path
+ *   gain_sums      device [B, d] fp32 or NULL; sums of a sample run in a fixed order
+ * d <= 16384, B * T < 2^31. */
+typedef struct {
+  const void*  h;
+  const void*  dy;
+  const void*  dh_in;
+  const float* gain;
+  void*        dh;
+  void*        dx;
+  float*       gain_sums;
+  int64_t h_row_stride, dy_row_stride, dh_in_row_stride, dh_row_stride, dx_row_stride;
+} adloco_norm_backward_io;
+int adloco_rms_norm_backward(adloco_ctx* ctx, const adloco_norm_backward_io* io, int64_t B, int64_t T, int32_t d,
+                             int dtype, double eps, const adloco_dropout_mask* mask, void* stream);
 
 /* Library version (major*10000 + minor*100 + patch). */
 int adloco_version(void);

@@ -21,7 +21,8 @@ int adloco_set_tuning(adloco_ctx* ctx, const char* name, int value);
 
 /* Measurement aid.  After adloco_set_tuning(ctx, "profile", 1) every launch of the named
  * kernel ("gram", "wgrad", "finalize", "sqnorm", "outer_step", "merge", "vector_table",
- * "inner_step", "inner_products", "tile_stats") is bracketed by HIP
+ * "inner_step", "inner_products", "tile_stats", "dropout", "rms_norm", "rms_norm_backward",
+ * "pack_blocks", "block_product") is bracketed by HIP
  * events on the call's stream.  adloco_profile_read waits for the recorded events of that
  * kernel, returns their summed duration in milliseconds and their count, and forgets them. */
 int adloco_profile_read(adloco_ctx* ctx, const char* kernel, double* total_ms, int* launches);

@@ -16,7 +16,7 @@ ADLOCO_F32, ADLOCO_BF16, ADLOCO_F16 = 0, 1, 2
 ADLOCO_ACCUMULATE = 0x1
 ADLOCO_SUM_ONLY = 0x2
 ADLOCO_GRAD_PROVIDED = 0x1
-ADLOCO_KIND_LINEAR, ADLOCO_KIND_VECTOR, ADLOCO_KIND_EMBED = 0x00, 0x10, 0x20
+ADLOCO_KIND_LINEAR, ADLOCO_KIND_VECTOR, ADLOCO_KIND_EMBED, ADLOCO_KIND_SAMPLE_SUMS = 0x00, 0x10, 0x20, 0x30
 ADLOCO_BROADCAST = 0x1
 ADLOCO_BIASED_VAR = 0x1
 ADLOCO_ALLOW_SHRINK = 0x2
@@ -37,6 +37,28 @@ class LinearDesc(C.Structure):
                 ("d_out", C.c_int32), ("a_row_stride", C.c_int64),
                 ("delta_row_stride", C.c_int64), ("grad_sum", C.c_void_p),
                 ("flags", C.c_uint32), ("reserved", C.c_uint32)]
+
+
+class DropoutMask(C.Structure):
+    _fields_ = [("p", C.c_double), ("seed", C.c_uint64), ("first_row", C.c_int64)]
+
+
+class Blocks8Desc(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("exponent", C.c_void_p), ("rows", C.c_int64), ("cols", C.c_int64),
+                ("row_stride", C.c_int64), ("exponent_stride", C.c_int64)]
+
+
+class NormIo(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("residual", C.c_void_p), ("gain", C.c_void_p), ("h", C.c_void_p),
+                ("y", C.c_void_p), ("x_row_stride", C.c_int64), ("residual_row_stride", C.c_int64),
+                ("h_row_stride", C.c_int64), ("y_row_stride", C.c_int64)]
+
+
+class NormBackwardIo(C.Structure):
+    _fields_ = [("h", C.c_void_p), ("dy", C.c_void_p), ("dh_in", C.c_void_p), ("gain", C.c_void_p),
+                ("dh", C.c_void_p), ("dx", C.c_void_p), ("gain_sums", C.c_void_p), ("h_row_stride", C.c_int64),
+                ("dy_row_stride", C.c_int64), ("dh_in_row_stride", C.c_int64), ("dh_row_stride", C.c_int64),
+                ("dx_row_stride", C.c_int64)]
 
 
 class StatsAcc(C.Structure):
@@ -163,13 +185,21 @@ def load_library():
                                               i64, i64, i32, i64, C.POINTER(IpTestResult), vp]
     lib.adloco_inner_product_decide.argtypes = [dbl, dbl, dbl, dbl, i64, dbl, dbl, i64, i64, i32,
                                                 i64, C.POINTER(IpTestResult)]
+    lib.adloco_dropout.argtypes = [vp, vp, i64, vp, i64, vp, i64, i64, i32, C.c_int, C.POINTER(DropoutMask), vp]
+    lib.adloco_pack_blocks.argtypes = [vp, vp, i64, i64, i64, C.c_int, C.POINTER(Blocks8Desc), C.POINTER(Blocks8Desc), vp]
+    lib.adloco_block_product.argtypes = [vp, C.POINTER(Blocks8Desc), C.POINTER(Blocks8Desc), vp, i64, C.c_int, u32, vp]
+    lib.adloco_rms_norm.argtypes = [vp, C.POINTER(NormIo), i64, i32, C.c_int, dbl, C.POINTER(DropoutMask),
+                                    C.POINTER(Blocks8Desc), vp]
+    lib.adloco_rms_norm_backward.argtypes = [vp, C.POINTER(NormBackwardIo), i64, i64, i32, C.c_int, dbl,
+                                             C.POINTER(DropoutMask), vp]
     lib.adloco_check_merge.argtypes = [C.POINTER(i64), C.c_int, C.c_int, C.POINTER(C.c_int),
                                        C.POINTER(C.c_int)]
     for name in ("adloco_create", "adloco_destroy", "adloco_set_tuning", "adloco_grad_stats",
                  "adloco_norm_test", "adloco_norm_test_noalloc", "adloco_norm_test_decide", "adloco_switch_mode",
                  "adloco_outer_step", "adloco_merge", "adloco_check_merge", "adloco_inner_step", "adloco_round",
                  "adloco_inner_products", "adloco_inner_product_test", "adloco_inner_product_decide",
-                 "adloco_pack_drift", "adloco_outer_step_drift", "adloco_merge_drift"):
+                 "adloco_pack_drift", "adloco_outer_step_drift", "adloco_merge_drift", "adloco_dropout",
+                 "adloco_pack_blocks", "adloco_block_product", "adloco_rms_norm", "adloco_rms_norm_backward"):
         getattr(lib, name).restype = C.c_int
     _lib = lib
     return lib
@@ -263,6 +293,8 @@ def make_layer_descs(layers: Sequence[dict], B: int, T: int, dtype: int):
     """layers: dicts with a [B,T,d_in], delta [B,T,d_out], optional grad_sum [d_out,d_in] fp32,
     optional provided=True.  Token rows may be strided views (last dim contiguous).
     kind="vector": a bias / gain block, delta [B,T,d], optional x [B,T,d], grad_sum [d].
+    kind="sample_sums": a vector block whose per-sample gradients are formed already, sums fp32 [B,d]
+    (samples may be a stride apart), grad_sum [d].
     kind="embed": an embedding table, ids int32 [B,T], delta [B,T,d], vocab=V, grad_sum [V,d]
     (maintained by the caller)."""
     import torch
@@ -278,11 +310,21 @@ def make_layer_descs(layers: Sequence[dict], B: int, T: int, dtype: int):
 
     for i, l in enumerate(layers):
         kind = l.get("kind", "linear")
-        d = l["delta"]
-        check_rows(i, "delta", d)
         g = l.get("grad_sum")
         flags = ADLOCO_GRAD_PROVIDED if l.get("provided") else 0
-        if kind == "linear":
+        if kind == "sample_sums":
+            d = l["sums"]
+            if not d.is_cuda or d.dtype != torch.float32 or d.dim() != 2 or d.shape[0] != B or d.stride(1) != 1:
+                raise ValueError(f"layer {i}: sums must be a GPU fp32 tensor [B={B},d] with unit stride in d, got "
+                                 f"{tuple(d.shape)} {d.dtype}")
+            d = d.unsqueeze(1)
+        else:
+            d = l["delta"]
+            check_rows(i, "delta", d)
+        if kind == "sample_sums":
+            a_ptr, a_stride, d_in, gshape = None, 0, 1, (d.shape[2],)
+            flags |= ADLOCO_KIND_SAMPLE_SUMS
+        elif kind == "linear":
             a = l["a"]
             check_rows(i, "a", a)
             a_ptr, a_stride, d_in, gshape = a.data_ptr(), a.stride(1), a.shape[2], (d.shape[2], a.shape[2])
@@ -313,7 +355,7 @@ def make_layer_descs(layers: Sequence[dict], B: int, T: int, dtype: int):
         arr[i].d_in = d_in
         arr[i].d_out = d.shape[2]
         arr[i].a_row_stride = a_stride
-        arr[i].delta_row_stride = d.stride(1)
+        arr[i].delta_row_stride = d.stride(0) if kind == "sample_sums" and B > 1 else d.stride(1) if kind != "sample_sums" else 0
         arr[i].grad_sum = g.data_ptr() if g is not None else None
         arr[i].flags = flags
         arr[i].reserved = 0
@@ -340,6 +382,9 @@ def adloco_grad_stats(ctx: Context, layers: Sequence[dict], B: int, T: int, dtyp
                                                 _stream_ptr(stream)))
 
 
+_VECTOR_KINDS = {"vector": ADLOCO_KIND_VECTOR, "sample_sums": ADLOCO_KIND_SAMPLE_SUMS}
+
+
 def _grad_sum_descs(layers):
     """Descriptors that carry only grad_sum, its shape and the block kind."""
     arr = (LinearDesc * len(layers))()
@@ -348,9 +393,9 @@ def _grad_sum_descs(layers):
         _dev_ptr(g, None, None, f"layer {i} grad_sum")
         arr[i].grad_sum = g.data_ptr()
         kind = l.get("kind", "linear")
-        if kind == "vector":
+        if kind in ("vector", "sample_sums"):
             arr[i].d_out, arr[i].d_in = g.shape[0], 1
-            arr[i].flags = ADLOCO_KIND_VECTOR | (ADLOCO_GRAD_PROVIDED if l.get("provided") else 0)
+            arr[i].flags = _VECTOR_KINDS[kind] | (ADLOCO_GRAD_PROVIDED if l.get("provided") else 0)
         elif kind == "embed":
             arr[i].d_in, arr[i].d_out = g.shape
             arr[i].flags = ADLOCO_KIND_EMBED | ADLOCO_GRAD_PROVIDED
@@ -538,6 +583,178 @@ def adloco_merge_drift(ctx: Context, x_rep, drifts, w_rep: float, w_others, stre
                                                  float(w_rep), w, len(drifts), N, _stream_ptr(stream)))
 
 
+class Blocks8:
+    """A matrix in 8-bit blocks of 128 (include/adloco.h: adloco_blocks8): data uint8 [rows, >= cols up to a multiple
+    of 128], exponent uint8 [ceil(cols / 128), >= rows].  Rows of both may be a stride apart, a multiple of 16."""
+
+    __slots__ = ("data", "exponent", "rows", "cols")
+
+    def __init__(self, data, exponent, rows: int, cols: int):
+        self.data, self.exponent, self.rows, self.cols = data, exponent, int(rows), int(cols)
+
+    @classmethod
+    def empty(cls, rows: int, cols: int, device="cuda"):
+        import torch
+        wide = -(-cols // 128) * 128
+        return cls(torch.empty((rows, wide), dtype=torch.uint8, device=device),
+                   torch.empty((wide // 128, -(-rows // 16) * 16), dtype=torch.uint8, device=device), rows, cols)
+
+
+def _on(ctx: Context, t, name: str):
+    if not t.is_cuda or t.device.index != ctx.device:
+        raise ValueError(f"{name} must live on the context's GPU, cuda:{ctx.device}")
+
+
+def _layer_stream(ctx: Context, stream):
+    import torch
+    return C.c_void_p((torch.cuda.current_stream(ctx.device) if stream is None else stream).cuda_stream)
+
+
+def _blocks8(ctx: Context, b: Optional[Blocks8], name: str):
+    """Descriptor of a Blocks8, or None."""
+    import torch
+    if b is None:
+        return None
+    for t, nm, rows, width in ((b.data, "data", b.rows, -(-b.cols // 128) * 128), (b.exponent, "exponent", -(-b.cols // 128), b.rows)):
+        _on(ctx, t, f"{name}.{nm}")
+        if t.dtype != torch.uint8 or t.dim() != 2 or t.shape[0] < rows or t.shape[1] < width or (t.shape[1] > 1 and t.stride(1) != 1):
+            raise ValueError(f"{name}.{nm} must be uint8 [>= {rows}, >= {width}] with unit stride along its rows, got "
+                             f"{tuple(t.shape)} {t.dtype}")
+    return Blocks8Desc(b.data.data_ptr(), b.exponent.data_ptr(), b.rows, b.cols,
+                       b.data.stride(0) if b.data.shape[0] > 1 else b.data.shape[1],
+                       b.exponent.stride(0) if b.exponent.shape[0] > 1 else b.exponent.shape[1])
+
+
+def _matrix(ctx: Context, t, name: str, like=None):
+    """(address, row stride) of a tensor [..., d] whose rows are a uniform stride apart; (None, 0) for None.  like: a
+    tensor whose shape and type it must have."""
+    if t is None:
+        return None, 0
+    _on(ctx, t, name)
+    if t.dim() < 1 or (like is not None and (t.shape != like.shape or t.dtype != like.dtype)):
+        raise ValueError(f"{name} must be {'a matrix' if like is None else f'{tuple(like.shape)} {like.dtype}'}, got "
+                         f"{tuple(t.shape)} {t.dtype}")
+    if t.is_contiguous():
+        return t.data_ptr(), t.shape[-1]
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name} needs unit stride in its last dimension")
+    stride = rows = None
+    for i in range(t.dim() - 2, -1, -1):          # the dimensions before the last walk over evenly spaced rows
+        if t.shape[i] == 1:
+            continue
+        if stride is None:
+            stride, rows = t.stride(i), t.shape[i]
+        elif t.stride(i) != stride * rows:
+            raise ValueError(f"{name}: its rows must be evenly spaced")
+        else:
+            rows *= t.shape[i]
+    return t.data_ptr(), t.shape[-1] if stride is None else stride
+
+
+_LAYER_DTYPES = {}
+
+
+def _layer_dtype(t, name: str) -> int:
+    import torch
+    if not _LAYER_DTYPES:
+        _LAYER_DTYPES.update({torch.float32: ADLOCO_F32, torch.bfloat16: ADLOCO_BF16, torch.float16: ADLOCO_F16})
+    code = _LAYER_DTYPES.get(t.dtype)
+    if code is None:
+        raise TypeError(f"{name} has dtype {t.dtype}, expected float32, bfloat16 or float16")
+    return code
+
+
+def _rows(t) -> int:
+    return t.numel() // t.shape[-1] if t.shape[-1] else 0
+
+
+def _mask(p: float, seed: int, first_row: int):
+    return DropoutMask(float(p), int(seed) & 0xFFFFFFFFFFFFFFFF, int(first_row)) if p else None
+
+
+def _gain(ctx: Context, gain, d: int):
+    import torch
+    if gain is None:
+        return None
+    _on(ctx, gain, "gain")
+    if gain.dtype != torch.float32 or gain.numel() != d or not gain.is_contiguous():
+        raise ValueError(f"gain must be a contiguous fp32 tensor of {d} values")
+    return gain.data_ptr()
+
+
+def adloco_dropout(ctx: Context, x, out, p: float, seed: int, first_row: int = 0, residual=None, stream=None):
+    """out = residual + dropout(x) (or dropout(x)); tensors [..., d] of one shape and type.  out may be x or residual.
+    The mask of a row depends on seed, its number first_row + i and the column alone: the same call on a gradient is the
+    backward pass."""
+    code = _layer_dtype(x, "x")
+    px, sx = _matrix(ctx, x, "x")
+    pr, sr = _matrix(ctx, residual, "residual", x)
+    po, so = _matrix(ctx, out, "out", x)
+    mask = DropoutMask(float(p), int(seed) & 0xFFFFFFFFFFFFFFFF, int(first_row))
+    ctx._check(load_library().adloco_dropout(ctx._h, px, sx, pr, sr, po, so, _rows(x), x.shape[-1], code, C.byref(mask),
+                                             _layer_stream(ctx, stream)))
+
+
+def adloco_pack_blocks(ctx: Context, x, along: Optional[Blocks8] = None, across: Optional[Blocks8] = None, stream=None):
+    """x [..., cols] to 8-bit blocks along its rows (along: rows x cols) and / or across them (across: cols x rows)."""
+    code = _layer_dtype(x, "x")
+    px, sx = _matrix(ctx, x, "x")
+    al, ac = _blocks8(ctx, along, "along"), _blocks8(ctx, across, "across")
+    ctx._check(load_library().adloco_pack_blocks(ctx._h, px, sx, _rows(x), x.shape[-1], code, al, ac,
+                                                 _layer_stream(ctx, stream)))
+
+
+def adloco_block_product(ctx: Context, a: Blocks8, b: Blocks8, out, flags: int = 0, stream=None):
+    """out [a.rows, b.rows] (fp32, bf16 or fp16) = a b^T; with ADLOCO_ACCUMULATE (fp32) added to out."""
+    code = _layer_dtype(out, "out")
+    da, db = _blocks8(ctx, a, "a"), _blocks8(ctx, b, "b")
+    if out.shape[-1] != b.rows or out.numel() != a.rows * b.rows:
+        raise ValueError(f"out must be [{a.rows}, {b.rows}], got {tuple(out.shape)}")
+    po, so = _matrix(ctx, out, "out")
+    ctx._check(load_library().adloco_block_product(ctx._h, da, db, po, so, code, flags, _layer_stream(ctx, stream)))
+
+
+def adloco_rms_norm(ctx: Context, x, gain, eps: float, y=None, y8: Optional[Blocks8] = None, residual=None, h_out=None,
+                    p: float = 0.0, seed: int = 0, first_row: int = 0, stream=None):
+    """h_out = h = residual + dropout(x); y (and y8, in 8-bit blocks) = h / sqrt(mean(h^2) + eps) * gain.  Tensors
+    [..., d] of one shape and type, gain fp32 [d] or None; outputs that are None are not written."""
+    code = _layer_dtype(x, "x")
+    d = x.shape[-1]
+    io = NormIo()
+    io.gain = _gain(ctx, gain, d)
+    io.x, io.x_row_stride = _matrix(ctx, x, "x")
+    io.residual, io.residual_row_stride = _matrix(ctx, residual, "residual", x)
+    io.h, io.h_row_stride = _matrix(ctx, h_out, "h_out", x)
+    io.y, io.y_row_stride = _matrix(ctx, y, "y", x)
+    ctx._check(load_library().adloco_rms_norm(ctx._h, C.byref(io), _rows(x), d, code, eps, _mask(p, seed, first_row),
+                                              _blocks8(ctx, y8, "y8"), _layer_stream(ctx, stream)))
+
+
+def adloco_rms_norm_backward(ctx: Context, h, gain, dy, eps: float, dh_out=None, gain_sums=None, dh_in=None, dx_out=None,
+                             p: float = 0.0, seed: int = 0, first_row: int = 0, stream=None):
+    """Gradient of the norm: dh_out = dh_in + d y / d h^T dy, dx_out = dropout(dh_out), gain_sums fp32 [B, d] = the gain's
+    gradient of every sample, whose rows are h's in order (B divides their number; None: one sample)."""
+    import torch
+    code = _layer_dtype(h, "h")
+    d, rows = h.shape[-1], _rows(h)
+    B = 1
+    io = NormBackwardIo()
+    if gain_sums is not None:
+        _on(ctx, gain_sums, "gain_sums")
+        B = gain_sums.shape[0]
+        if gain_sums.dtype != torch.float32 or tuple(gain_sums.shape) != (B, d) or not gain_sums.is_contiguous() or (B and rows % B):
+            raise ValueError(f"gain_sums must be a contiguous fp32 tensor [B, {d}] with B dividing {rows} rows")
+        io.gain_sums = gain_sums.data_ptr()
+    io.gain = _gain(ctx, gain, d)
+    io.h, io.h_row_stride = _matrix(ctx, h, "h")
+    io.dy, io.dy_row_stride = _matrix(ctx, dy, "dy", h)
+    io.dh_in, io.dh_in_row_stride = _matrix(ctx, dh_in, "dh_in", h)
+    io.dh, io.dh_row_stride = _matrix(ctx, dh_out, "dh_out", h)
+    io.dx, io.dx_row_stride = _matrix(ctx, dx_out, "dx_out", h)
+    ctx._check(load_library().adloco_rms_norm_backward(ctx._h, C.byref(io), B, rows // B if B else 0, d, code, eps,
+                                                       _mask(p, seed, first_row), _layer_stream(ctx, stream)))
+
+
 def adloco_check_merge(b_req: Sequence[int], w: int):
     k = len(b_req)
     arr = (C.c_int64 * max(k, 1))(*[int(v) for v in b_req])
@@ -556,9 +773,9 @@ def adloco_round(ctx: Context, cfg: dict, trainers: Sequence[dict], blocks: Sequ
     trainers: dicts {theta_outer, momentum, b_req, acc, per_sample_sqnorm, uid, workers: [{theta,
     exp_avg, exp_avg_sq, grad, step}]} of GPU tensors; updated in place (b_req, step); the list is
     reordered / shortened like the C array when trainers merge.
-    blocks: template of the parameter blocks: dicts {d_in, d_out, kind ("linear" | "vector")}.
+    blocks: template of the parameter blocks: dicts {d_in, d_out, kind ("linear" | "vector" | "sample_sums")}.
     batch_fn(uid, worker, inner_step, micro_step, b, theta_ptr) -> list of dicts {a | x, delta}
-    (GPU tensors [b, T, .]) in block order; the tensors are kept alive until the round returns.
+    (GPU tensors [b, T, .]; for sample_sums {sums}, fp32 [b, d]) in block order; the tensors are kept alive until the round returns.
     Returns the reports of the remaining trainers."""
     import torch
     lib = load_library()
@@ -567,9 +784,9 @@ def adloco_round(ctx: Context, cfg: dict, trainers: Sequence[dict], blocks: Sequ
     N = 0
     for l, b in enumerate(blocks):
         kind = b.get("kind", "linear")
-        tmpl[l].d_in = 1 if kind == "vector" else b["d_in"]
+        tmpl[l].d_in = 1 if kind in _VECTOR_KINDS else b["d_in"]
         tmpl[l].d_out = b["d_out"]
-        tmpl[l].flags = ADLOCO_KIND_VECTOR if kind == "vector" else 0
+        tmpl[l].flags = _VECTOR_KINDS.get(kind, 0)
         N += tmpl[l].d_in * tmpl[l].d_out
     k = len(trainers)
     arr = (Trainer * k)()
@@ -604,8 +821,11 @@ def adloco_round(ctx: Context, cfg: dict, trainers: Sequence[dict], blocks: Sequ
             keep_alive.append(got)
             for l in range(n):
                 e = got[l]
-                d = e["delta"]
                 desc = layers[l]        # (every index makes a ctypes object of its own)
+                if "sums" in e:
+                    desc.delta = _dev_ptr(e["sums"], torch.float32, int(b) * desc.d_out, "sums").value
+                    continue
+                d = e["delta"]
                 desc.delta = d.data_ptr()
                 desc.delta_row_stride = d.stride(1)
                 x = e.get("a") if "a" in e else e.get("x")

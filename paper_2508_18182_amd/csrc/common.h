@@ -354,6 +354,7 @@ struct adloco_ctx {
   bool ip_any_rest = false;
   int ip_rest_group = 1;
   int ip_group_tuning = 0;     // 0: cost model; else samples per tile entry
+  adloco::Scratch layer_part;  // partial sums of the layer operators: one block of a fixed size, never moved
   // statistics by per-sample gradient tiles: of the blocks whose gradient sum is formed here, or of all if none is.
   // Built with the layer table; a list for which there is no memory is missing, and its routes with it.
   adloco::TileList tiles16;    // aligned 16-bit blocks
@@ -411,7 +412,8 @@ inline int fail(adloco_ctx* ctx, int code, const char* fmt, ...) {
 
 // Event timing of one kernel launch when ctx->profile is set (no-ops otherwise).
 enum ProfKernel { kProfGram = 0, kProfWgrad, kProfFinalize, kProfSqnorm, kProfOuter, kProfMerge,
-                  kProfVecTab, kProfInner, kProfIp, kProfTileStats, kProfCount };
+                  kProfVecTab, kProfInner, kProfIp, kProfTileStats, kProfDropout, kProfNorm, kProfNormBack, kProfPack,
+                  kProfProduct, kProfCount };
 hipEvent_t prof_begin(adloco_ctx* ctx, hipStream_t st);
 void prof_end(adloco_ctx* ctx, int kernel, hipEvent_t start, hipStream_t st);
 

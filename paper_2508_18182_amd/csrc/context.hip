@@ -67,7 +67,8 @@ using namespace adloco;
 
 static const char* const kProfNames[kProfCount] = {"gram", "wgrad", "finalize", "sqnorm",
                                                    "outer_step", "merge", "vector_table",
-                                                   "inner_step", "inner_products", "tile_stats"};
+                                                   "inner_step", "inner_products", "tile_stats", "dropout", "rms_norm",
+                                                   "rms_norm_backward", "pack_blocks", "block_product"};
 
 extern "C" int adloco_profile_read(adloco_ctx* ctx, const char* kernel, double* total_ms,
                                    int* launches) {
@@ -151,7 +152,7 @@ extern "C" int adloco_destroy(adloco_ctx* ctx) {
                     &ctx->order_tab, &ctx->group_tab, &ctx->job_tab, &ctx->wgx_tab,
                     &ctx->wgx_split, &ctx->wgx_part, &ctx->vec_tab, &ctx->emb_tab,
                     &ctx->aux_vec, &ctx->aux_perm, &ctx->aux_part, &ctx->ip_tab, &ctx->ip_tile_out,
-                    &ctx->ip_dot, &ctx->ip_sq, &ctx->ip_flags, &ctx->tile_out};
+                    &ctx->ip_dot, &ctx->ip_sq, &ctx->ip_flags, &ctx->tile_out, &ctx->layer_part};
   for (Scratch* s : all)
     if (s->ptr) (void)hipFree(s->ptr);
   for (TileList* p : {&ctx->tiles16, &ctx->tiles32[0], &ctx->tiles32[1], &ctx->ip_rest[0], &ctx->ip_rest[1]})

@@ -115,9 +115,10 @@ int prepare_tables(adloco_ctx* ctx, const adloco_linear_desc* layers, int n_laye
       return fail(ctx, ADLOCO_EINVAL, "layer %d: unknown flags or non-zero reserved field", l);
     const bool provided = d.flags & ADLOCO_GRAD_PROVIDED;
     const int kind = int(d.flags & ADLOCO_KIND_MASK);
-    if (kind != ADLOCO_KIND_LINEAR && kind != ADLOCO_KIND_VECTOR && kind != ADLOCO_KIND_EMBED)
+    const bool sums = kind == ADLOCO_KIND_SAMPLE_SUMS, vector = kind == ADLOCO_KIND_VECTOR || sums;
+    if (kind != ADLOCO_KIND_LINEAR && !vector && kind != ADLOCO_KIND_EMBED)
       return fail(ctx, ADLOCO_EINVAL, "layer %d: unknown kind 0x%x", l, kind);
-    if (kind == ADLOCO_KIND_VECTOR && d.d_in != 1)
+    if (vector && d.d_in != 1)
       return fail(ctx, ADLOCO_EINVAL, "layer %d: a vector block needs d_in = 1", l);
     if (kind == ADLOCO_KIND_EMBED && !provided)
       return fail(ctx, ADLOCO_EINVAL, "layer %d: an embedding block needs ADLOCO_GRAD_PROVIDED", l);
@@ -125,20 +126,21 @@ int prepare_tables(adloco_ctx* ctx, const adloco_linear_desc* layers, int n_laye
     L.a = d.a;
     L.delta = d.delta;
     L.grad_sum = d.grad_sum;
-    L.a_stride = d.a_row_stride ? d.a_row_stride : (kind == ADLOCO_KIND_VECTOR ? d.d_out : d.d_in);
+    L.a_stride = d.a_row_stride ? d.a_row_stride : (vector ? d.d_out : d.d_in);
     L.delta_stride = d.delta_row_stride ? d.delta_row_stride : d.d_out;
     L.d_in = d.d_in;
     L.d_out = d.d_out;
     L.provided = provided ? 1 : 0;
     L.kind = kind;
     if (need_inputs) {
-      if (!d.delta || (!d.a && kind != ADLOCO_KIND_VECTOR))
+      if (!d.delta || (!d.a && !vector))
         return fail(ctx, ADLOCO_EINVAL, "layer %d: a or delta is NULL", l);
+      if (d.a && sums) return fail(ctx, ADLOCO_EINVAL, "layer %d: a block of per-sample sums takes no a", l);
       const long long a_width = kind == ADLOCO_KIND_LINEAR ? d.d_in : d.d_out;
       if ((kind != ADLOCO_KIND_EMBED && d.a && L.a_stride < a_width) || L.delta_stride < d.d_out)
         return fail(ctx, ADLOCO_EINVAL, "layer %d: row stride smaller than the row", l);
       const size_t a_esize = kind == ADLOCO_KIND_EMBED ? 4 : esize;
-      if ((reinterpret_cast<uintptr_t>(d.a) % a_esize) || (reinterpret_cast<uintptr_t>(d.delta) % esize))
+      if ((reinterpret_cast<uintptr_t>(d.a) % a_esize) || (reinterpret_cast<uintptr_t>(d.delta) % (sums ? 4 : esize)))
         return fail(ctx, ADLOCO_EINVAL, "layer %d: a or delta not aligned to its element size", l);
       if (!provided && !d.grad_sum)
         return fail(ctx, ADLOCO_EINVAL, "layer %d: grad_sum is NULL without ADLOCO_GRAD_PROVIDED", l);
@@ -362,9 +364,10 @@ int prepare_vector_table(adloco_ctx* ctx, int B, int T, hipStream_t st) {
     if (L.kind == ADLOCO_KIND_LINEAR) continue;
     AuxDesc A{};
     A.layer = int(l);
-    const int w = L.kind == ADLOCO_KIND_VECTOR ? slab : embed_table_slab();
+    const bool vector = L.kind == ADLOCO_KIND_VECTOR || L.kind == ADLOCO_KIND_SAMPLE_SUMS;
+    const int w = vector ? slab : embed_table_slab();
     A.slabs = (L.d_out + w - 1) / w;
-    if (L.kind == ADLOCO_KIND_VECTOR) {
+    if (vector) {
       A.blk_start = int(vb);
       A.blk_start2 = int(vb2);
       A.vec_off = voff;

@@ -1,0 +1,180 @@
+// Device arithmetic shared by the layer operators: rows of eight values, the dropout mask, 8-bit blocks.
+#pragma once
+
+#include "common.h"
+
+namespace adloco {
+
+// ---- eight consecutive values of a row -----------------------------------------------------------------------------
+// FAST: rows are 16-byte aligned and whole multiples of eight long, so that a lane's eight are all there or all not.
+template <typename E, bool FAST> __device__ __forceinline__ void load_eight(const E* row, int c, int d, float (&v)[8]) {
+  typedef __attribute__((ext_vector_type(8))) E vec;
+  if constexpr (FAST) {
+    if (c < d) {
+      const vec r = __builtin_nontemporal_load(reinterpret_cast<const vec*>(row + c));
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = float(r[j]);
+      return;
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = 0.f;
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = c + j < d ? float(row[c + j]) : 0.f;
+  }
+}
+template <typename E, bool FAST> __device__ __forceinline__ void store_eight(E* row, int c, int d, const float (&v)[8]) {
+  typedef __attribute__((ext_vector_type(8))) E vec;
+  if constexpr (FAST) {
+    if (c < d) {
+      vec r;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) r[j] = E(v[j]);
+      __builtin_nontemporal_store(r, reinterpret_cast<vec*>(row + c));
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (c + j < d) row[c + j] = E(v[j]);
+  }
+}
+
+// ---- dropout -------------------------------------------------------------------------------------------------------
+// Philox4x32-10 (Salmon, Moraes, Dror, Shaw, "Parallel random numbers: as easy as 1, 2, 3", 2011): ten rounds of two
+// 32 x 32 -> 64 bit products each turn a counter and a key into 128 random bits.  Eight columns of a row take one counter
+// (column / 8, row, row >> 32, 0) and 16 bits each: the mask of an element depends on its row number and column alone,
+// whatever the launch, so that it is formed again in the backward pass and never stored.  16 bits instead of 32 halve the
+// integer work, which otherwise takes longer than the memory traffic of a 16-bit tensor.
+struct DropoutArgs {
+  unsigned k0, k1;           // key: the seed
+  unsigned threshold;        // dropped below it; 0: no dropout
+  float scale;               // 65536 / (65536 - threshold)
+  unsigned long long first_row;
+};
+__device__ __forceinline__ void drop_eight(const DropoutArgs& m, long long row, int c, float (&v)[8]) {
+  const unsigned long long r = m.first_row + (unsigned long long)row;
+  unsigned c0 = unsigned(c) >> 3, c1 = unsigned(r), c2 = unsigned(r >> 32), c3 = 0;
+  unsigned k0 = m.k0, k1 = m.k1;
+#pragma unroll
+  for (int i = 0; i < 10; ++i) {
+    const unsigned long long p0 = (unsigned long long)c0 * 0xD2511F53u, p1 = (unsigned long long)c2 * 0xCD9E8D57u;
+    c0 = unsigned(p1 >> 32) ^ c1 ^ k0;
+    c1 = unsigned(p1);
+    c2 = unsigned(p0 >> 32) ^ c3 ^ k1;
+    c3 = unsigned(p0);
+    k0 += 0x9E3779B9u;
+    k1 += 0xBB67AE85u;
+  }
+  const unsigned w[4] = {c0, c1, c2, c3};
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const unsigned u = (j & 1) ? w[j >> 1] >> 16 : w[j >> 1] & 0xffffu;
+    v[j] = u < m.threshold ? 0.f : v[j] * m.scale;        // (selected, not multiplied: a dropped NaN is gone)
+  }
+}
+
+// ---- 8-bit blocks --------------------------------------------------------------------------------------------------
+// |x|, or 0 where x is not finite (those become NaN below and have no say in the block's exponent).
+__device__ __forceinline__ float finite_abs(float x) {
+  const float a = fabsf(x);
+  return a <= 3.402823466e38f ? a : 0.f;
+}
+// Biased exponent of the smallest power of two s >= 2^-126 with big <= 448 s, 448 = 1.75 * 2^8 the largest e4m3 value: read
+// off the bits of `big`, hence exact.
+__device__ __forceinline__ unsigned block_exponent(float big) {
+  const unsigned b = __float_as_uint(big);
+  const int e = int(b >> 23) - 8 + ((b & 0x7fffffu) > 0x600000u ? 1 : 0);
+  return unsigned(e < 1 ? 1 : e);
+}
+__device__ __forceinline__ float block_inverse(unsigned exponent) { return __uint_as_float((254u - exponent) << 23); }
+// Eight values times `inv` (a power of two, hence exact) to e4m3, round to nearest even: at most half a step, 2^-4 of a
+// value that is not below 2^-6.  The largest is 448 by the choice of the exponent, so that nothing saturates.
+__device__ __forceinline__ uint2 pack_eight(const float (&v)[8], float inv) {
+  uint2 out;
+  unsigned* o = &out.x;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    int w = 0;
+    w = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * h] * inv, v[4 * h + 1] * inv, w, false);
+    w = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * h + 2] * inv, v[4 * h + 3] * inv, w, true);
+    unsigned u = unsigned(w);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (!(fabsf(v[4 * h + j]) <= 3.402823466e38f)) u |= 0x7fu << (8 * j);     // infinities too: e4m3 has none
+    o[h] = u;
+  }
+  return out;
+}
+// Maximum over groups of 16 lanes, in all of them.  Every lane of the wave has to be there.
+__device__ __forceinline__ float max16(float v) {
+#define ADLOCO_ROR_MAX(n) \
+  v = fmaxf(v, __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), 0x120 + n, 0xf, 0xf, false)))
+  ADLOCO_ROR_MAX(8);
+  ADLOCO_ROR_MAX(4);
+  ADLOCO_ROR_MAX(2);
+  ADLOCO_ROR_MAX(1);
+#undef ADLOCO_ROR_MAX
+  return v;
+}
+__device__ __forceinline__ float sum64(float v) {
+#define ADLOCO_ROR_ADD(n) \
+  v += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), 0x120 + n, 0xf, 0xf, false))
+  ADLOCO_ROR_ADD(8);
+  ADLOCO_ROR_ADD(4);
+  ADLOCO_ROR_ADD(2);
+  ADLOCO_ROR_ADD(1);
+#undef ADLOCO_ROR_ADD
+  v += __shfl_xor(v, 16, 64);
+  v += __shfl_xor(v, 32, 64);
+  return v;
+}
+
+// ---- host side -----------------------------------------------------------------------------------------------------
+// The context's device made current for a call, the caller's restored behind it.
+class DeviceScope {
+ public:
+  explicit DeviceScope(const adloco_ctx* ctx) {
+    int now = -1;
+    if (hipGetDevice(&now) == hipSuccess && now != ctx->device) {
+      before_ = now;
+      ok_ = hipSetDevice(ctx->device) == hipSuccess;
+    }
+  }
+  ~DeviceScope() {
+    if (before_ >= 0) (void)hipSetDevice(before_);
+  }
+  DeviceScope(const DeviceScope&) = delete;
+  DeviceScope& operator=(const DeviceScope&) = delete;
+  bool ok() const { return ok_; }
+
+ private:
+  int before_ = -1;
+  bool ok_ = true;
+};
+
+// One matrix argument as the checks see it: `rows` rows of `width` bytes, `stride` bytes apart.
+struct RowSpan {
+  const void* p;
+  long long rows, width, stride;
+  bool same(const RowSpan& o) const { return p == o.p && (stride == o.stride || rows <= 1); }
+};
+// Whether two of them may share a byte.  Column ranges of one buffer (equal strides) do not.
+inline bool spans_overlap(const RowSpan& x, const RowSpan& y) {
+  if (!x.p || !y.p || x.rows <= 0 || y.rows <= 0) return false;
+  const uintptr_t a = reinterpret_cast<uintptr_t>(x.p), b = reinterpret_cast<uintptr_t>(y.p);
+  const uintptr_t ae = a + uintptr_t((x.rows - 1) * x.stride + x.width), be = b + uintptr_t((y.rows - 1) * y.stride + y.width);
+  if (ae <= b || be <= a) return false;
+  if (x.stride != y.stride || x.stride <= 0) return true;
+  const uintptr_t s = uintptr_t(x.stride), off = a <= b ? (b - a) % s : (s - (a - b) % s) % s;   // of y's rows within x's
+  return off < uintptr_t(x.width) || s - off < uintptr_t(y.width);
+}
+
+// Scratch of the layer operators: one block of a fixed size, taken by the first call that needs it and never moved, so
+// that captured calls keep it.  NULL if there is none and the stream is being captured, or there is no memory.
+constexpr size_t kLayerScratch = size_t(64) << 20;
+inline float* layer_scratch(adloco_ctx* ctx, hipStream_t st) {
+  return obtain_scratch(ctx, ctx->layer_part, kLayerScratch, st) ? static_cast<float*>(ctx->layer_part.ptr) : nullptr;
+}
+const char* check_blocks8(const adloco_blocks8* b);
+
+}  // namespace adloco

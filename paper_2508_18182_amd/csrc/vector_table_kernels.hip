@@ -91,6 +91,11 @@ __global__ __launch_bounds__(kVtThreads) void vector_rowsum_kernel(const LayerDe
   const int rel = blockIdx.x - A.blk_start;
   const int sample = rel / A.slabs, slab = rel % A.slabs;
   const int d = L.d_out;
+  if (L.kind == ADLOCO_KIND_SAMPLE_SUMS) {        // summed over t already, in fp32
+    const int col = slab * kSlab + threadIdx.x;
+    if (col < d) vec[A.vec_off + (long long)sample * d + col] = static_cast<const float*>(L.delta)[sample * L.delta_stride + col];
+    return;
+  }
   const int cs = threadIdx.x & 31, rg = threadIdx.x >> 5;
   const int c = slab * kSlab + cs * 8;
   const E* D = reinterpret_cast<const E*>(L.delta) + (long long)sample * T * L.delta_stride;

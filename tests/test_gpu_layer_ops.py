@@ -1,0 +1,480 @@
+"""The layer operators -- dropout, residual RMS norm, 8-bit blocks and their product -- through the public entry points
+against the fp64 oracle.
+
+Tolerances.  u = 2^-24 is the largest relative error of one fp32 operation; half(E) = eps / 2 that of the last rounding.
+  dropout       x * scale: scale and product rounded, 2 u |x s|; the sum u |h|; the store half(E) |h|.
+  norm          h as above; the sum of squares is 64 terms in a row and 8 in a tree, all positive: 72 u of it, half of that
+                after the root, plus four more roundings: y is off by 64 u |y| at most, by what h's own error does to it,
+                and by half(E) |y|.
+  blocks        2^-4 of a value (half a step of 3 mantissa bits), 2^-10 of the block's power of two below its normal range.
+  backward      w - n mean(w n): 64 + 8 terms again, r, n and the products: (80 u) (|w| + |n| mean|w n|) r, then the sums.
+  gain sums     T terms of one sample, in runs: (T + 16) u sum |dy n|, n itself off by 64 u.
+  product       K products, exact, summed in some order with errors of 2 u each (matrix instructions may cut off):
+                2 K u sum |a b|; and exactly where every partial sum is a whole number below 2^24."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2508_18182_amd as A
+from oracle import layer_oracle as lo
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0**-24
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+DEV = "cuda:0"
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = A.Context(0)
+    yield c
+    c.close()
+
+
+def half(dtype):
+    return torch.finfo(dtype).eps / 2
+
+
+def tiny(dtype):
+    return torch.finfo(dtype).smallest_normal * torch.finfo(dtype).eps
+
+
+def rand(seed, shape, dtype, std=1.0):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(shape, generator=g) * std).to(dtype).to(DEV)
+
+
+def host(t):
+    return t.detach().cpu().double().numpy()
+
+
+def apart(t, pad, offset=0):
+    """The same values as a view whose rows are `pad` elements further apart, `offset` elements into the buffer."""
+    rows, d = t.shape
+    buf = torch.full((rows * (d + pad) + offset + pad,), 7.0, dtype=t.dtype, device=t.device)
+    v = buf[offset:offset + rows * (d + pad)].view(rows, d + pad)[:, :d]
+    v.copy_(t)
+    return v, buf
+
+
+def close(got, want, tol):
+    got, want = host(got) if isinstance(got, torch.Tensor) else got, np.asarray(want)
+    bad = np.abs(got - want) > tol
+    assert not bad.any(), (int(bad.sum()), np.argwhere(bad)[:3].tolist(), got[bad][:3], want[bad][:3])
+
+
+# ---- dropout --------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("rows,d", [(1, 1), (3, 7), (1, 8), (64, 768), (5, 1025), (1000, 64), (2, 40000)])
+def test_dropout(ctx, rows, d, dtype):
+    dt = TYPES[dtype]
+    x, res = rand(1, (rows, d), dt), rand(2, (rows, d), dt, 3.0)
+    p, seed = 0.3, 0xFEDCBA9876543210
+    xs = np.abs(lo.dropout(host(x), p, seed, 5))
+    for r in (None, res):
+        out = torch.full_like(x, 9.0)
+        A.adloco_dropout(ctx, x, out, p, seed, first_row=5, residual=r)
+        want = lo.dropout(host(x), p, seed, 5) + (0 if r is None else host(r))
+        close(out, want, half(dt) * np.abs(want) * (1 + 1e-6) + 3 * U * xs + 2 * U * np.abs(want) + tiny(dt))
+    y = x.clone()                                      # in place, and as its own backward pass
+    A.adloco_dropout(ctx, y, y, p, seed, first_row=5)
+    assert torch.equal((y == 0) | (x == 0), torch.from_numpy(~lo.dropout_keep(rows, d, p, seed, 5)).to(DEV) | (x == 0))
+    r = res.clone()
+    A.adloco_dropout(ctx, x, r, p, seed, first_row=5, residual=r)
+    assert torch.equal(r, out)
+
+
+def test_dropout_edges(ctx):
+    x = rand(3, (6, 96), torch.float32)
+    out = torch.empty_like(x)
+    A.adloco_dropout(ctx, x, out, 0.0, 1)              # nothing dropped: the very values
+    assert torch.equal(out, x)
+    bad = torch.full_like(x, float("nan"))
+    A.adloco_dropout(ctx, bad, out, 0.5, 7)
+    keep = torch.from_numpy(lo.dropout_keep(6, 96, 0.5, 7)).to(DEV)
+    assert torch.equal(torch.isnan(out), keep) and bool((out[~keep] == 0).all())
+    A.adloco_dropout(ctx, x, out, 65535 / 65536, 7)    # nearly all dropped
+    assert torch.equal(out != 0, torch.from_numpy(lo.dropout_keep(6, 96, 65535 / 65536, 7)).to(DEV))
+    big = 2**40 + 3                                    # rows whose number passes 32 bits
+    A.adloco_dropout(ctx, x, out, 0.5, 2**63 + 1, first_row=big)
+    assert torch.equal(out != 0, torch.from_numpy(lo.dropout_keep(6, 96, 0.5, 2**63 + 1, big)).to(DEV))
+    A.adloco_dropout(ctx, x[:0], out[:0], 0.5, 1)      # no rows
+
+
+@pytest.mark.parametrize("pad,offset", [(8, 0), (1, 0), (8, 1), (0, 3)])
+def test_dropout_of_strided_rows_leaves_the_rest(ctx, pad, offset):
+    x, _ = apart(rand(4, (9, 72), torch.bfloat16), pad, offset)
+    out, buf = apart(torch.zeros(9, 72, dtype=torch.bfloat16, device=DEV), pad, offset)
+    plain = torch.empty(9, 72, dtype=torch.bfloat16, device=DEV)
+    A.adloco_dropout(ctx, x, out, 0.2, 11)
+    A.adloco_dropout(ctx, x.contiguous(), plain, 0.2, 11)
+    assert torch.equal(out, plain)
+    out.fill_(7.0)
+    assert bool((buf == 7).all())
+
+
+# ---- 8-bit blocks ---------------------------------------------------------------------------
+
+def codes_of(b):
+    """(values, exponents) of a Blocks8 on the host, the padding among them."""
+    wide = -(-b.cols // 128) * 128
+    return lo.e4m3_table()[b.data[:, :wide].cpu().numpy()], b.exponent[:, :b.rows].cpu().numpy()
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("rows,cols", [(1, 1), (1, 128), (3, 129), (127, 8), (128, 128), (129, 130), (300, 65), (16, 1000)])
+def test_pack_blocks(ctx, rows, cols, dtype):
+    x = rand(rows * 1000 + cols, (rows, cols), TYPES[dtype], 0.02)
+    x[0, 0] = 0
+    along, across = A.Blocks8.empty(rows, cols, DEV), A.Blocks8.empty(cols, rows, DEV)
+    for b in (along, across):
+        b.data.fill_(0x55)
+    A.adloco_pack_blocks(ctx, x, along, across)
+    for b, v in ((along, host(x)), (across, host(x).T)):
+        got, want = codes_of(b), lo.pack(v)
+        np.testing.assert_array_equal(got[1], want[1])
+        np.testing.assert_array_equal(got[0], want[0])
+    for one in ("along", "across"):                    # asked for by itself: the same
+        b = A.Blocks8.empty(*((rows, cols) if one == "along" else (cols, rows)), DEV)
+        A.adloco_pack_blocks(ctx, x, **{one: b})
+        both = along if one == "along" else across
+        assert torch.equal(b.data, both.data) and torch.equal(b.exponent[:, :b.rows], both.exponent[:, :b.rows])
+
+
+def test_pack_blocks_extremes(ctx):
+    x = torch.zeros(8, 256, device=DEV)
+    x[0, :5] = torch.tensor([3.4028234e38, 1.0, -3.4028234e38, 1e30, -1e36])
+    x[1, :4] = torch.tensor([1e-45, -1e-40, 1e-38, 2.0**-135])
+    x[2, 7] = float("inf")
+    x[2, 8] = -2.5
+    x[3, 130], x[3, 131] = float("nan"), float("-inf")
+    x[4, :6] = torch.tensor([448.0, 449.0, 460.0, -448.0, 0.5, 2.0**-12])
+    x[5, 0] = -0.0
+    x[6] = 2.0**-126
+    along, across = A.Blocks8.empty(8, 256, DEV), A.Blocks8.empty(256, 8, DEV)
+    A.adloco_pack_blocks(ctx, x, along, across)
+    for b, v in ((along, host(x)), (across, host(x).T)):
+        got, want = codes_of(b), lo.pack(v)
+        np.testing.assert_array_equal(got[1], want[1])
+        np.testing.assert_array_equal(got[0], want[0])
+
+
+def test_pack_blocks_of_views(ctx):
+    x = rand(5, (140, 200), torch.float16)
+    want = A.Blocks8.empty(140, 200, DEV), A.Blocks8.empty(200, 140, DEV)
+    A.adloco_pack_blocks(ctx, x, *want)
+    for pad, offset in ((8, 0), (3, 0), (8, 1)):
+        v, _ = apart(x, pad, offset)
+        wide = torch.full((150, 512), 0x33, dtype=torch.uint8, device=DEV)
+        exps = torch.full((6, 192), 0x44, dtype=torch.uint8, device=DEV)
+        along = A.Blocks8(wide[:, 128:], exps[2:, 16:], 140, 200)        # inside larger buffers
+        across = A.Blocks8.empty(200, 140, DEV)
+        A.adloco_pack_blocks(ctx, v, along, across)
+        assert torch.equal(along.data[:140, :256], want[0].data) and torch.equal(along.exponent[:2, :140], want[0].exponent[:, :140])
+        assert torch.equal(across.data, want[1].data)
+        wide[:140, 128:384] = 0x33
+        exps[2:4, 16:156] = 0x44
+        assert bool((wide == 0x33).all()) and bool((exps == 0x44).all())
+
+
+def random_blocks(seed, rows, cols, whole=False):
+    """Blocks8 of random codes and exponents (whole: small whole numbers, all powers of two 1), and what it stands for."""
+    r = np.random.default_rng(seed)
+    b = A.Blocks8.empty(rows, cols, DEV)
+    b.data.zero_()
+    if whole:
+        v = torch.from_numpy(r.integers(-8, 9, (rows, cols))).float().to(torch.float8_e4m3fn).view(torch.uint8)
+        e = torch.full((b.exponent.shape[0], rows), 127, dtype=torch.uint8)
+    else:
+        v = torch.from_numpy(r.normal(size=(rows, cols)) * 60).float().clamp(-448, 448).to(torch.float8_e4m3fn).view(torch.uint8)
+        e = torch.from_numpy(r.integers(110, 130, (b.exponent.shape[0], rows))).to(torch.uint8)
+    b.exponent.fill_(255)                              # behind the last row: never to be used
+    b.data[:, :cols] = v.to(DEV)
+    b.exponent[:, :rows] = e.to(DEV)
+    return b, lo.unpack(b.data.cpu().numpy(), b.exponent[:, :rows].cpu().numpy(), cols)
+
+
+PRODUCTS = [(1, 1, 1), (1, 130, 257), (3, 64, 128), (16, 96, 640), (17, 33, 100), (40, 500, 1000), (65, 64, 384), (128, 128, 128),
+            (129, 257, 513), (130, 1000, 250), (300, 300, 1500), (513, 260, 700), (64, 72, 20000), (256, 256, 9000), (1000, 31, 128),
+            (2, 3000, 2000), (31, 129, 40000)]
+
+
+@pytest.mark.parametrize("m,n,k", PRODUCTS)
+def test_block_product_of_whole_numbers_is_exact(ctx, m, n, k):
+    (a, av), (b, bv) = random_blocks(m + n, m, k, True), random_blocks(k, n, k, True)
+    want = av @ bv.T                                   # |partial sums| <= 64 K < 2^24 up to K = 262144
+    out = torch.full((m, n), float("nan"), device=DEV)
+    A.adloco_block_product(ctx, a, b, out)
+    np.testing.assert_array_equal(host(out), want)
+    base = torch.from_numpy(np.random.default_rng(1).integers(-1000, 1000, (m, n))).float().to(DEV)
+    acc = base.clone()
+    A.adloco_block_product(ctx, a, b, acc, A.ADLOCO_ACCUMULATE)
+    np.testing.assert_array_equal(host(acc), want + host(base))
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("m,n,k", [(1, 70, 300), (33, 129, 1000), (129, 260, 513), (300, 300, 4000)])
+def test_block_product(ctx, m, n, k, dtype):
+    dt = TYPES[dtype]
+    (a, av), (b, bv) = random_blocks(m + n, m, k), random_blocks(k, n, k)
+    scale = 2.0**-6 if dtype == "f16" else 1.0         # (within the type's range: 448 * 448 * 2^6 * sqrt(K) is not)
+    if dtype == "f16":
+        a.exponent[:, :m] -= 9
+        b.exponent[:, :n] -= 9
+        av, bv = av * 2.0**-9, bv * 2.0**-9
+    want, size = av @ bv.T, np.abs(av) @ np.abs(bv).T
+    out = torch.full((m, n), float("nan"), dtype=dt, device=DEV)
+    A.adloco_block_product(ctx, a, b, out)
+    close(out, want, half(dt) * np.abs(want) + 2 * k * U * size * (1 + half(dt)) + tiny(dt))
+    again = torch.empty_like(out)
+    A.adloco_block_product(ctx, a, b, again)
+    assert torch.equal(out, again)                     # a fixed order of summation
+    view, buf = apart(torch.zeros_like(out), 5, 3)
+    A.adloco_block_product(ctx, a, b, view)
+    assert torch.equal(view, out)
+    view.fill_(7.0)
+    assert bool((buf == 7).all())
+
+
+def test_block_product_of_sliced_operands(ctx):
+    (a, av), (b, bv) = random_blocks(1, 96, 640, True), random_blocks(2, 80, 640, True)
+    sa = A.Blocks8(a.data[16:], a.exponent[:, 16:], 70, 640)            # rows 16 .. 85
+    sb = A.Blocks8(b.data[:, 128:], b.exponent[1:], 80, 500)            # columns 128 .. 627
+    sa = A.Blocks8(sa.data[:, 128:], sa.exponent[1:], 70, 500)
+    a.data[:, 628:] = 0
+    out = torch.empty(70, 80, device=DEV)
+    A.adloco_block_product(ctx, sa, sb, out)
+    np.testing.assert_array_equal(host(out), av[16:86, 128:628] @ bv[:, 128:628].T)
+
+
+def test_block_product_nan_stays_in_its_row(ctx):
+    (a, av), (b, bv) = random_blocks(3, 200, 300, True), random_blocks(4, 150, 300, True)
+    a.data[77, 123] = 0x7F
+    b.data[99, 5] = 0xFF
+    out = torch.empty(200, 150, device=DEV)
+    A.adloco_block_product(ctx, a, b, out)
+    want = av @ bv.T
+    want[77], want[:, 99] = np.nan, np.nan
+    np.testing.assert_array_equal(host(out), want)
+
+
+# ---- norm -----------------------------------------------------------------------------------
+
+def norm_inputs(rows, d, dt, seed=0):
+    x, res = rand(seed + 1, (rows, d), dt), rand(seed + 2, (rows, d), dt, 4.0)
+    gain = 1 + 0.1 * rand(seed + 3, (d,), torch.float32)
+    return x, res, gain
+
+
+def norm_tolerance(h, err, gain, eps, y):
+    """What an error of h (elementwise bound err) and the fp32 arithmetic do to y."""
+    rms = np.sqrt((h * h).mean(1, keepdims=True) + eps)
+    return np.abs(host(gain)) / rms * err + np.abs(y) * (64 * U + np.sqrt((err * err).mean(1, keepdims=True)) / rms)
+
+
+WIDTHS = [1, 7, 8, 64, 130, 512, 520, 768, 1024, 1100, 2048, 2056, 4096, 5000, 8192, 8200, 16384]
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("d", WIDTHS)
+def test_rms_norm(ctx, d, dtype):
+    dt, rows, eps, p, seed = TYPES[dtype], 5, 1e-5, 0.25, 99
+    x, res, gain = norm_inputs(rows, d, dt, d)
+    for drop in (0.0, p):
+        for r in (None, res):
+            h = lo.dropout(host(x), drop, seed) + (0 if r is None else host(r))
+            err = 3 * U * np.abs(lo.dropout(host(x), drop, seed)) + 2 * U * np.abs(h)
+            want = lo.rms_norm(h, host(gain), eps)
+            off = norm_tolerance(h, err, gain, eps, want)
+            y, h_out, y8 = torch.full_like(x, 9.0), torch.full_like(x, 9.0), A.Blocks8.empty(rows, d, DEV)
+            y8.data.fill_(0x55)
+            A.adloco_rms_norm(ctx, x, gain, eps, y=y, y8=y8, residual=r, h_out=h_out, p=drop, seed=seed)
+            close(h_out, h, half(dt) * np.abs(h) * (1 + 1e-6) + err + tiny(dt))
+            close(y, want, half(dt) * np.abs(want) * (1 + 1e-4) + off + tiny(dt))
+            check_y8(y8, want, off)
+            only = A.Blocks8.empty(rows, d, DEV)       # each output by itself is the same
+            A.adloco_rms_norm(ctx, x, gain, eps, y8=only, residual=r, p=drop, seed=seed)
+            assert torch.equal(only.data, y8.data) and torch.equal(only.exponent[:, :rows], y8.exponent[:, :rows])
+            alone = torch.empty_like(y)
+            A.adloco_rms_norm(ctx, x, gain, eps, y=alone, residual=r, p=drop, seed=seed)
+            assert torch.equal(alone, y)
+
+
+def check_y8(y8, want, off):
+    rows, d = want.shape
+    codes, exps = codes_of(y8)
+    blocks = exps.shape[0]
+    pad = np.zeros((rows, blocks * 128))
+    pad[:, :d] = np.abs(want)
+    slack = np.zeros_like(pad)
+    slack[:, :d] = off
+    least = lo.block_exponent(np.maximum(pad - slack, 0).reshape(rows, blocks, 128).max(2)).T
+    most = lo.block_exponent((pad + slack).reshape(rows, blocks, 128).max(2)).T
+    assert ((exps >= least) & (exps <= most)).all()
+    assert not codes[:, d:].any()
+    power = np.exp2(exps.astype(np.float64) - 127).T
+    got = (codes * np.repeat(power, 128, axis=1))[:, :d]
+    power = np.repeat(power, 128, axis=1)[:, :d]
+    tol = 2.0**-4 * np.abs(want) + 2.0**-10 * power + off * (1 + 2.0**-4)
+    assert (np.abs(got - want) <= tol).all()
+
+
+@pytest.mark.parametrize("rows", [1, 2, 31, 4096, 5001])
+def test_rms_norm_row_counts(ctx, rows):
+    d = 264
+    x, res, gain = norm_inputs(rows, d, torch.bfloat16)
+    want = lo.rms_norm(host(x) + host(res), host(gain), 1e-6)
+    h = host(x) + host(res)
+    y, y8 = torch.empty_like(x), A.Blocks8.empty(rows, d, DEV)
+    A.adloco_rms_norm(ctx, x, gain, 1e-6, y=y, y8=y8, residual=res)
+    off = norm_tolerance(h, 5 * U * np.abs(h), gain, 1e-6, want)
+    close(y, want, half(torch.bfloat16) * np.abs(want) * (1 + 1e-4) + off)
+    check_y8(y8, want, off)
+
+
+def test_rms_norm_without_gain_in_place_and_strided(ctx):
+    x, res, gain = norm_inputs(20, 136, torch.float16)
+    ones = torch.ones(136, device=DEV)
+    a, b = torch.empty_like(x), torch.empty_like(x)
+    A.adloco_rms_norm(ctx, x, None, 1e-5, y=a)
+    A.adloco_rms_norm(ctx, x, ones, 1e-5, y=b)
+    assert torch.equal(a, b)
+    h, y = torch.empty_like(x), torch.empty_like(x)
+    A.adloco_rms_norm(ctx, x, gain, 1e-5, y=y, residual=res, h_out=h, p=0.1, seed=4)
+    xx, rr = x.clone(), res.clone()
+    A.adloco_rms_norm(ctx, xx, gain, 1e-5, y=xx, residual=rr, h_out=rr, p=0.1, seed=4)
+    assert torch.equal(xx, y) and torch.equal(rr, h)
+    for pad, offset in ((8, 0), (1, 0), (8, 1)):
+        (xv, _), (rv, _) = apart(x, pad, offset), apart(res, pad, offset)
+        (hv, hb), (yv, yb) = apart(torch.zeros_like(x), pad, offset), apart(torch.zeros_like(x), pad, offset)
+        A.adloco_rms_norm(ctx, xv, gain, 1e-5, y=yv, residual=rv, h_out=hv, p=0.1, seed=4)
+        assert torch.equal(yv, y) and torch.equal(hv, h)
+        hv.fill_(7.0)
+        yv.fill_(7.0)
+        assert bool((hb == 7).all()) and bool((yb == 7).all())
+    A.adloco_rms_norm(ctx, x[:0], gain, 1e-5, y=y[:0])
+
+
+@pytest.mark.parametrize("d", [96, 3000])
+def test_rms_norm_rows_out_of_the_ordinary(ctx, d):
+    x = rand(8, (7, d), torch.float32)
+    x[0] = 0
+    x[1] *= 1e30                                       # squares beyond fp32
+    x[2] *= 1e-30                                      # squares below it: eps decides
+    x[3, 5] = float("inf")
+    x[4, 6] = float("nan")
+    x[5] = 3.0e38
+    gain = 1 + 0.1 * rand(9, (d,), torch.float32)
+    y, y8 = torch.empty_like(x), A.Blocks8.empty(7, d, DEV)
+    A.adloco_rms_norm(ctx, x, gain, 1e-5, y=y, y8=y8)
+    plain = [0, 1, 2, 5, 6]
+    want = lo.rms_norm(host(x)[plain], host(gain), 1e-5)
+    close(y[plain], want, 70 * U * np.abs(want) + 1e-44)
+    check_y8(A.Blocks8(y8.data[plain], y8.exponent[:, plain], 5, d), want, 70 * U * np.abs(want) + 1e-44)
+    inf, nan = host(y)[3], host(y)[4]                  # inf / inf, and finite values over an infinite norm
+    assert np.isnan(inf[5]) and not np.delete(inf, 5).any() and np.isnan(nan).all()
+    assert np.isnan(codes_of(y8)[0][4][:d]).all() and np.isnan(codes_of(y8)[0][3][5])
+    assert not codes_of(y8)[0][:, d:].any()
+
+
+BACK = [(1, 1, 1), (1, 3, 7), (3, 1, 64), (2, 9, 130), (4, 16, 512), (1, 100, 768), (3, 41, 1030), (2, 64, 2048), (70, 1, 300),
+        (1, 5, 2056), (2, 17, 4100), (1, 9, 8192), (2, 3, 16384), (1, 2000, 72)]
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("B,T,d", BACK)
+def test_rms_norm_backward(ctx, B, T, d, dtype):
+    dt, eps, p, seed = TYPES[dtype], 1e-5, 0.25, 12345678901234
+    rows = B * T
+    h, dy, dh_in = rand(1, (rows, d), dt, 2.0), rand(2, (rows, d), dt), rand(3, (rows, d), dt)
+    gain = 1 + 0.1 * rand(4, (d,), torch.float32)
+    grad, parts = lo.rms_norm_backward(host(h), host(gain), host(dy), eps)
+    r = 1 / np.sqrt((host(h)**2).mean(1, keepdims=True) + eps)
+    n, w = host(h) * r, host(gain) * host(dy)
+    err = 80 * U * r * (np.abs(w) + np.abs(n) * np.abs(w * n).mean(1, keepdims=True))
+    sums = parts.reshape(B, T, d).sum(1)
+    sums_tol = (T + 80) * U * np.abs(parts).reshape(B, T, d).sum(1)
+    for extra in (None, dh_in):
+        dh, dx = torch.full_like(h, 9.0), torch.full_like(h, 9.0)
+        gs = torch.full((B, d), 9.0, device=DEV)
+        A.adloco_rms_norm_backward(ctx, h, gain, dy, eps, dh, gain_sums=gs, dh_in=extra, dx_out=dx, p=p, seed=seed)
+        want = grad + (0 if extra is None else host(extra))
+        e = err + 2 * U * np.abs(want)
+        close(dh, want, half(dt) * np.abs(want) * (1 + 1e-4) + e + tiny(dt))
+        drop = lo.dropout(want, p, seed)
+        scale = 65536 / (65536 - lo.dropout_threshold(p))
+        close(dx, drop, half(dt) * np.abs(drop) * (1 + 1e-4) + 2 * scale * e + 3 * U * np.abs(drop) + tiny(dt))
+        close(gs, sums, sums_tol)
+    # what is not asked for changes nothing; dx without dropout is dh
+    only, same = torch.empty_like(h), torch.empty_like(h)
+    A.adloco_rms_norm_backward(ctx, h, gain, dy, eps, only, dh_in=dh_in)
+    assert torch.equal(only, dh)
+    A.adloco_rms_norm_backward(ctx, h, gain, dy, eps, dx_out=same, dh_in=dh_in)
+    assert torch.equal(same, dh)
+    gs2 = torch.empty_like(gs)
+    A.adloco_rms_norm_backward(ctx, h, gain, dy, eps, gain_sums=gs2)
+    assert torch.equal(gs2, gs)
+
+
+def test_rms_norm_backward_in_place_strided_and_empty(ctx):
+    rows, d = 30, 136
+    h, dy, dh_in = (rand(s, (rows, d), torch.bfloat16) for s in (1, 2, 3))
+    dh, dx = torch.empty_like(h), torch.empty_like(h)
+    A.adloco_rms_norm_backward(ctx, h, None, dy, 1e-5, dh, dh_in=dh_in, dx_out=dx, p=0.1, seed=3)
+    a, b = dh_in.clone(), dy.clone()
+    A.adloco_rms_norm_backward(ctx, h, None, b, 1e-5, a, dh_in=a, dx_out=b, p=0.1, seed=3)
+    assert torch.equal(a, dh) and torch.equal(b, dx)
+    for pad, offset in ((8, 0), (1, 0), (8, 1)):
+        hv, yv, iv = (apart(t, pad, offset)[0] for t in (h, dy, dh_in))
+        (ov, ob), (xv, xb) = apart(torch.zeros_like(h), pad, offset), apart(torch.zeros_like(h), pad, offset)
+        A.adloco_rms_norm_backward(ctx, hv, None, yv, 1e-5, ov, dh_in=iv, dx_out=xv, p=0.1, seed=3)
+        assert torch.equal(ov, dh) and torch.equal(xv, dx)
+        ov.fill_(7.0)
+        xv.fill_(7.0)
+        assert bool((ob == 7).all()) and bool((xb == 7).all())
+    gs = torch.full((3, d), 5.0, device=DEV)           # samples without a row: sums of nothing
+    A.adloco_rms_norm_backward(ctx, h[:0], None, dy[:0], 1e-5, dh[:0], gain_sums=gs)
+    assert not bool(gs.any())
+
+
+@pytest.mark.parametrize("d", [96, 3000])
+def test_rms_norm_backward_of_large_rows(ctx, d):
+    h, dy = rand(8, (4, d), torch.float32), rand(9, (4, d), torch.float32)
+    h[0] *= 1e30
+    h[1] = 0
+    h[2] *= 1e-30
+    dh, gs = torch.empty_like(h), torch.empty(4, d, device=DEV)
+    A.adloco_rms_norm_backward(ctx, h, None, dy, 1e-5, dh, gain_sums=gs)
+    grad, parts = lo.rms_norm_backward(host(h), np.ones(d), host(dy), 1e-5)
+    close(gs, parts, 90 * U * np.abs(parts) + 1e-44)
+    r = 1 / np.sqrt((host(h)**2).mean(1, keepdims=True) + 1e-5)
+    n = host(h) * r
+    close(dh, grad, 90 * U * r * (np.abs(host(dy)) + np.abs(n) * np.abs(host(dy) * n).mean(1, keepdims=True)) + 1e-44)
+
+
+def test_gradient_against_differences_of_the_kernel(ctx):
+    """The backward kernel against differences of the forward kernel (fp32, a loss of fixed weights): central differences
+    with step s are off by s^2 / 6 of the third derivative and by the rounding of two losses over 2 s."""
+    rows, d, eps, s = 2, 24, 1e-2, 2.0**-5
+    h, dy, gain = rand(1, (rows, d), torch.float32), rand(2, (rows, d), torch.float32), 1 + 0.1 * rand(3, (d,), torch.float32)
+    dh, gs = torch.empty_like(h), torch.empty(rows, d, device=DEV)
+    A.adloco_rms_norm_backward(ctx, h, gain, dy, eps, dh, gain_sums=gs)
+    y = torch.empty_like(h)
+
+    def loss(hh, gg):
+        A.adloco_rms_norm(ctx, hh, gg, eps, y=y)
+        return float((y.double() * dy.double()).sum())
+
+    for c in range(0, d, 5):
+        a, b = h.clone(), h.clone()
+        a[1, c] += s
+        b[1, c] -= s
+        diff = (loss(a, gain) - loss(b, gain)) / (2 * s)
+        assert abs(diff - float(dh[1, c])) < 4e-3 * (1 + abs(diff))          # s^2 = 1e-3 times derivatives of order one
+        a, b = gain.clone(), gain.clone()
+        a[c] += s
+        b[c] -= s
+        diff = (loss(h, a) - loss(h, b)) / (2 * s)                            # linear in the gain: rounding only
+        assert abs(diff - float(gs[:, c].sum())) < 1e-4 * (1 + abs(diff))
