@@ -1,5 +1,7 @@
 // 8-bit blocks: packing of a matrix along its rows and / or across them, and the product of two packed matrices on the
 // scaled matrix instructions.
+#include <type_traits>
+
 #include "layer_ops.h"
 
 namespace adloco {
@@ -99,10 +101,21 @@ template <typename E, bool FAST> __global__ __launch_bounds__(256) void pack_blo
 
 // ---------------------------------------------------------------------------------------------------------------------
 // Product.  out[m][n] = sum_k 2^(ea[k / 128][m] - 127) 2^(eb[k / 128][n] - 127) a[m][k] b[n][k]: both operands hold k
-// contiguously.  One v_mfma_scale_f32_16x16x128 multiplies 16 rows by 16 columns over one block of 128 and applies the two
-// powers of two by itself; products are exact, sums in fp32.  Which 32 of the 128 values of k a lane holds does not matter
-// as long as both operands agree; which 16 rows make a block of the tile is free too, and a lane takes neighbouring rows
-// for the blocks (row = lane * MB + block), so that their exponents are one load and a lane's outputs of a row one store.
+// contiguously.
+//   16-bit outputs: one v_mfma_scale_f32_16x16x128 multiplies 16 rows by 16 columns over one block of 128 and applies the
+// two powers of two by itself.  It adds its products in groups whose members it cuts off below 2^-13 of the largest of them
+// (measured; the unscaled 8-bit instructions do the same), which leaves 1.5e-5 of a sum of Gaussian values: a hundredth of
+// what the output's own rounding costs in bf16, a tenth in fp16.
+//   fp32 outputs (EXACT): gradient sums would keep that error, so the values are widened to bf16 in registers, where they and
+// their powers of two are exact, and multiplied by v_mfma_f32_16x16x32_bf16 at half the rate: products exact, sums fp32.
+// Which 32 of the 128 values of k a lane holds does not matter as long as both operands agree; which 16 rows make a block of
+// the tile is free too, and a lane takes neighbouring rows for the blocks (row = lane * NB + block), so that their exponents
+// are one load and a lane's outputs of a row one store.
+//   A workgroup of four waves forms a tile of 2 x 2 wave tiles of (16 NB)^2.  Blocks of k come by direct loads into one of two
+// LDS stages (rows of 128 bytes, 16-byte chunks permuted so that eight neighbouring rows lie in different banks).  Per
+// block: the rows of A stream through a few registers, those of B are held; once the last row of A has been read, the
+// workgroup meets, the stage just read takes the block after next, and the rows of B of the next block are fetched behind the
+// last products of this one.
 // ---------------------------------------------------------------------------------------------------------------------
 typedef __attribute__((ext_vector_type(8))) int mfma_i32x8;
 typedef __attribute__((ext_vector_type(4))) int i32x4;
@@ -111,74 +124,274 @@ struct ProductArgs {
   const unsigned char *a, *b, *ea, *eb;
   long long as, bs, eas, ebs;
   void* out;
+  float* part;                 // partial tiles [tile][piece] of a split contraction; NULL: none
   long long os;
   int M, N, steps;             // steps: blocks of k
-  int tiles_n;
-  int accumulate;
+  int tiles_m, tiles_n, pieces;
+  int accumulate, vec;         // vec: NB outputs of a row are one aligned store
 };
 
-template <typename E> __device__ __forceinline__ void put_out(E* p, float v, bool accumulate) {
-  if constexpr (std::is_same<E, float>::value) *p = accumulate ? *p + v : v;
-  else *p = E(v);
+constexpr int kTileGroup = 4;  // tile rows that an XCD walks down before it takes the next tile column
+
+// Tile and piece of a workgroup: consecutive workgroups go to the eight XCDs in turn, each XCD gets a contiguous run of the
+// tiles, in bands of kTileGroup tile rows, so that what shares an L2 shares rows of A and columns of B.
+__device__ __forceinline__ bool product_place(const ProductArgs& p, int& tm, int& tn, int& piece, int& tile) {
+  const int tiles = p.tiles_m * p.tiles_n, total = tiles * p.pieces, per = (total + kNumXcd - 1) / kNumXcd;
+  const int w = (blockIdx.x % kNumXcd) * per + blockIdx.x / kNumXcd;
+  if (int(blockIdx.x / kNumXcd) >= per || w >= total) return false;
+  tile = w / p.pieces;
+  piece = w - tile * p.pieces;
+  const int band = tile / (kTileGroup * p.tiles_n), first = band * kTileGroup;
+  const int high = p.tiles_m - first < kTileGroup ? p.tiles_m - first : kTileGroup;
+  const int in = tile - first * p.tiles_n;
+  tn = in / high;
+  tm = first + in - tn * high;
+  return true;
 }
 
-constexpr int kProductTile = 128;
+// 4 bytes per lane to LDS, consecutive (see direct_load_lds16).
+__device__ __forceinline__ void direct_load_lds4(const void* src, unsigned lds_addr) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(src), "s"(lds_addr) : "m0");
+}
 
-template <typename E> __global__ __launch_bounds__(256) void product_kernel(ProductArgs p) {
-  __shared__ __attribute__((aligned(16))) unsigned char lds[2][kProductTile * 128];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int l16 = lane & 15, kg = lane >> 4;
-  const long long m0 = (long long)(blockIdx.x / p.tiles_n) * kProductTile, n0 = (long long)(blockIdx.x % p.tiles_n) * kProductTile;
-  const int wm = (wave >> 1) * 64, wn = (wave & 1) * 64;
-  mfma_f32x4 acc[4][4] = {};
-  const long long ra = m0 + wm + l16 * 4 < p.M ? m0 + wm + l16 * 4 : 0, rb = n0 + wn + l16 * 4 < p.N ? n0 + wn + l16 * 4 : 0;
-  for (int s = 0; s < p.steps; ++s) {
-    __syncthreads();
+// The 32 values of a lane times their power of two, as four bf16 operands.
+struct WideFrag { mfma_bf16x8 k[4]; };
+__device__ __forceinline__ WideFrag widen(const mfma_i32x8& f, unsigned exponent) {
+  typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+  const float s = __uint_as_float(exponent << 23);
+  WideFrag w;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int r = (tid >> 3) + i * 32, ch = tid & 7;
-      const long long am = m0 + r < p.M ? m0 + r : p.M - 1, bn = n0 + r < p.N ? n0 + r : p.N - 1;
-      const int at = r * 128 + ((ch ^ ((r >> 2) & 7)) * 16);
-      *reinterpret_cast<i32x4*>(lds[0] + at) = *reinterpret_cast<const i32x4*>(p.a + am * p.as + (long long)s * 128 + ch * 16);
-      *reinterpret_cast<i32x4*>(lds[1] + at) = *reinterpret_cast<const i32x4*>(p.b + bn * p.bs + (long long)s * 128 + ch * 16);
+  for (int i = 0; i < 8; ++i) {
+    const bf16x2 lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(unsigned(f[i]), s, false);
+    const bf16x2 hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(unsigned(f[i]), s, true);
+    w.k[i / 2][(i & 1) * 4 + 0] = lo[0];
+    w.k[i / 2][(i & 1) * 4 + 1] = lo[1];
+    w.k[i / 2][(i & 1) * 4 + 2] = hi[0];
+    w.k[i / 2][(i & 1) * 4 + 3] = hi[1];
+  }
+  return w;
+}
+
+// PINNED: accumulators in the accumulation registers and in assembly, for tiles that need all of them (the compiler moves
+// them about otherwise, and spills).  Operands and exponents come straight from LDS, so that no vector instruction that wrote
+// them stands near; fences as for mfma_16x16x32.
+template <int SEL_A, int SEL_B, bool PINNED>
+__device__ __forceinline__ void scaled_mfma(mfma_f32x4& c, const mfma_i32x8& a, const mfma_i32x8& b, int ea, int eb) {
+  if constexpr (PINNED)
+    asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[%5,%6,0] op_sel_hi:[%7,%8,0]"
+                 : "+a"(c) : "v"(a), "v"(b), "v"(ea), "v"(eb), "n"(SEL_A & 1), "n"(SEL_B & 1), "n"(SEL_A >> 1), "n"(SEL_B >> 1));
+  else
+    c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, SEL_A, ea, SEL_B, eb);
+}
+template <int SEL_A, int NB>
+__device__ __forceinline__ void scaled_row(mfma_f32x4 (&c)[NB], const mfma_i32x8& a, const mfma_i32x8 (&b)[NB], int ea, const int (&eb)[NB / 4]) {
+#pragma unroll
+  for (int n = 0; n < NB; n += 4) {
+    scaled_mfma<SEL_A, 0, NB == 8>(c[n], a, b[n], ea, eb[n / 4]);
+    scaled_mfma<SEL_A, 1, NB == 8>(c[n + 1], a, b[n + 1], ea, eb[n / 4]);
+    scaled_mfma<SEL_A, 2, NB == 8>(c[n + 2], a, b[n + 2], ea, eb[n / 4]);
+    scaled_mfma<SEL_A, 3, NB == 8>(c[n + 3], a, b[n + 3], ea, eb[n / 4]);
+  }
+}
+
+template <typename E, int NB> __device__ __forceinline__ void store_row(E* p, const float (&v)[NB], int left, bool vec, bool accumulate) {
+  typedef __attribute__((ext_vector_type(NB))) E row;
+  if (vec && left >= NB) {
+    row r, old;
+    if constexpr (std::is_same<E, float>::value)
+      if (accumulate) old = *reinterpret_cast<const row*>(p);
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
+      if constexpr (std::is_same<E, float>::value) r[n] = accumulate ? old[n] + v[n] : v[n];
+      else r[n] = E(v[n]);
     }
-    const int ea = *reinterpret_cast<const int*>(p.ea + s * p.eas + ra), eb = *reinterpret_cast<const int*>(p.eb + s * p.ebs + rb);
-    __syncthreads();
-    mfma_i32x8 fa[4], fb[4];
+    *reinterpret_cast<row*>(p) = r;
+    return;
+  }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int x = wm + l16 * 4 + i, y = wn + l16 * 4 + i;
+  for (int n = 0; n < NB; ++n)
+    if (n < left) {
+      if constexpr (std::is_same<E, float>::value) p[n] = accumulate ? p[n] + v[n] : v[n];
+      else p[n] = E(v[n]);
+    }
+}
+
+template <int NB> struct TileShape {
+  static constexpr int wave = 16 * NB, edge = 2 * wave;
+  static constexpr int stage = 2 * edge * 128 + 2 * edge;      // A, B, their exponents
+  static constexpr int lds = 2 * stage;
+  static constexpr int resident = NB == 8 ? 1 : 2;             // workgroups per compute unit
+};
+
+template <int NB, bool EXACT, typename E>
+__global__ __launch_bounds__(256, TileShape<NB>::resident) void product_tile_kernel(ProductArgs p) {
+  constexpr int edge = TileShape<NB>::edge, wave_edge = TileShape<NB>::wave, stage = TileShape<NB>::stage;
+  extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+  int tm, tn, piece, tile;
+  if (!product_place(p, tm, tn, piece, tile)) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l16 = lane & 15, kg = lane >> 4;
+  const int m0 = tm * edge, n0 = tn * edge;
+  const int s0 = int((long long)p.steps * piece / p.pieces), s1 = int((long long)p.steps * (piece + 1) / p.pieces);
+  const unsigned at = lds_address(lds);
+
+  // Direct loads: a wave brings NB times eight rows of each operand.  Slot q of a stage holds row (q % 16) * NB + q / 16 of
+  // its wave tile (the 16 rows of a block side by side), chunk c of it at place c ^ (q % 8).
+  const int slot = wave * NB * 8 + (lane >> 3), chunk = ((lane & 7) ^ (lane >> 3)) * 16;
+  const int last_a = p.M - m0 - 1, last_b = p.N - n0 - 1;
+  auto row_offset = [&](int i, int last, int stride) {         // (rows behind the last one: the last one again)
+    const int q = slot + i * 8, in = q % wave_edge, r = q - in + (in & 15) * NB + (in >> 4);
+    return __umul24(unsigned(r < last ? r : last), unsigned(stride)) + chunk;
+  };
+  const unsigned char* base_a = uniform_ptr(p.a + (long long)m0 * p.as + (long long)s0 * 128);
+  const unsigned char* base_b = uniform_ptr(p.b + (long long)n0 * p.bs + (long long)s0 * 128);
+  // exponents, four rows a lane: wave 0 those of A and wave 1 those of B, or wave 0 both where 32 lanes are enough for each
+  const bool of_b = NB == 8 ? wave == 1 : lane >= 32;
+  const int er = (NB == 8 ? lane : lane & 31) * 4, rows = of_b ? p.N - n0 : p.M - m0;
+  const unsigned char* pe = (of_b ? p.eb + (long long)s0 * p.ebs + n0 : p.ea + (long long)s0 * p.eas + m0) + (er < rows ? er : 0);
+  const long long pe_step = of_b ? p.ebs : p.eas;
+  auto load = [&](int buf) {
+    const unsigned to = at + buf * stage + wave * (NB * 1024);
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const i32x4 u = *reinterpret_cast<const i32x4*>(lds[0] + x * 128 + (((kg * 2 + h) ^ ((x >> 2) & 7)) * 16));
-        const i32x4 w = *reinterpret_cast<const i32x4*>(lds[1] + y * 128 + (((kg * 2 + h) ^ ((y >> 2) & 7)) * 16));
+    for (int i = 0; i < NB; ++i) direct_load_lds16_s(row_offset(i, last_a, int(p.as)), base_a, to + i * 1024);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          fa[i][h * 4 + j] = u[j];
-          fb[i][h * 4 + j] = w[j];
+    for (int i = 0; i < NB; ++i) direct_load_lds16_s(row_offset(i, last_b, int(p.bs)), base_b, to + edge * 128 + i * 1024);
+    if (wave < (NB == 8 ? 2 : 1)) direct_load_lds4(pe, at + buf * stage + 2 * edge * 128 + (NB == 8 && wave == 1 ? edge : 0));
+    base_a += 128;
+    base_b += 128;
+    pe += pe_step;
+  };
+  auto meet = [&] {            // everything asked for is here, for all waves
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
+  const int wm = (wave >> 1) * wave_edge, wn = (wave & 1) * wave_edge;
+  const int key = l16 & 7;
+  const int row_a = (wm + l16) * 128, row_b = edge * 128 + (wn + l16) * 128;
+  const int c0 = ((kg * 2) ^ key) * 16, c1 = ((kg * 2 + 1) ^ key) * 16;
+  auto frag = [&](int buf, int row, int block) {
+    const unsigned char* q = lds + buf * stage + row + block * 2048;
+    const i32x4 x = *reinterpret_cast<const i32x4*>(q + c0), y = *reinterpret_cast<const i32x4*>(q + c1);
+    return mfma_i32x8{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+  };
+  struct Exps { int a[NB / 4], b[NB / 4]; };
+  auto exps = [&](int buf, Exps& e) {
+    const unsigned char* q = lds + buf * stage + 2 * edge * 128;
+#pragma unroll
+    for (int i = 0; i < NB / 4; ++i) {
+      e.a[i] = *reinterpret_cast<const int*>(q + wm + l16 * NB + i * 4);
+      e.b[i] = *reinterpret_cast<const int*>(q + edge + wn + l16 * NB + i * 4);
+    }
+  };
+
+  constexpr bool pinned = NB == 8 && !EXACT;
+  mfma_f32x4 acc[NB][NB] = {};
+  if constexpr (pinned) mfma_fence(acc);
+  struct Held { mfma_i32x8 b[NB], a0, a1; Exps e; };
+  constexpr int ahead = 2;                            // rows of A fetched before they are multiplied
+  auto fetch = [&](int buf, Held& h) {
+    exps(buf, h.e);
+#pragma unroll
+    for (int n = 0; n < NB; ++n) h.b[n] = frag(buf, row_b, n);
+    h.a0 = frag(buf, row_a, 0);
+    h.a1 = frag(buf, row_a, 1);
+  };
+  auto step = [&](int buf, bool more, bool load_next, Held& h, Held& next) {
+    mfma_i32x8 a[NB];
+    a[0] = h.a0;
+    a[1] = h.a1;
+    WideFrag wb[EXACT ? NB : 1];
+    if constexpr (EXACT)
+#pragma unroll
+      for (int n = 0; n < NB; ++n) wb[n] = widen(h.b[n], (unsigned(h.e.b[n / 4]) >> (8 * (n & 3))) & 255u);
+#pragma unroll
+    for (int m = 0; m < NB; ++m) {
+      if (m + ahead < NB) a[m + ahead] = frag(buf, row_a, m + ahead);
+      if (m == NB - ahead) {                          // the stage has been read by this wave
+        if (more) {
+          meet();
+          if (load_next) load(buf);
+          fetch(buf ^ 1, next);
         }
       }
-    }
-#define ADLOCO_STEP(m, n) \
-  acc[m][n] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fa[m], fb[n], acc[m][n], 0, 0, m, ea, n, eb)
-#define ADLOCO_ROW(m) ADLOCO_STEP(m, 0); ADLOCO_STEP(m, 1); ADLOCO_STEP(m, 2); ADLOCO_STEP(m, 3)
-    ADLOCO_ROW(0); ADLOCO_ROW(1); ADLOCO_ROW(2); ADLOCO_ROW(3);
-#undef ADLOCO_ROW
-#undef ADLOCO_STEP
-  }
-  E* out = static_cast<E*>(p.out);
+      if constexpr (EXACT) {
+        const WideFrag wa = widen(a[m], (unsigned(h.e.a[m / 4]) >> (8 * (m & 3))) & 255u);
 #pragma unroll
-  for (int m = 0; m < 4; ++m)
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+          for (int n = 0; n < NB; ++n) acc[m][n] = mfma_16x16x32_v<false>(wa.k[k], wb[n].k[k], acc[m][n]);
+      } else {
+        if (m % 4 == 0) scaled_row<0, NB>(acc[m], a[m], h.b, h.e.a[m / 4], h.e.b);
+        if (m % 4 == 1) scaled_row<1, NB>(acc[m], a[m], h.b, h.e.a[m / 4], h.e.b);
+        if (m % 4 == 2) scaled_row<2, NB>(acc[m], a[m], h.b, h.e.a[m / 4], h.e.b);
+        if (m % 4 == 3) scaled_row<3, NB>(acc[m], a[m], h.b, h.e.a[m / 4], h.e.b);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  load(0);
+  meet();
+  const int n = s1 - s0;                              // >= 1
+  if (n > 1) load(1);
+  Held h0, h1;
+  fetch(0, h0);
+  for (int s = 0; s < n; s += 2) {
+    step(0, s + 1 < n, s + 2 < n, h0, h1);
+    if (s + 1 < n) step(1, s + 2 < n, s + 3 < n, h1, h0);
+  }
+
+  if constexpr (pinned) mfma_fence(acc);
+  // element j of block (m, n): row (kg * 4 + j) * NB + m of the wave tile, column l16 * NB + n
+  if (p.part) {
+    float* to = p.part + ((long long)tile * p.pieces + piece) * (edge * edge) + wn + l16 * NB;
+#pragma unroll
+    for (int m = 0; m < NB; ++m)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        float v[NB];
+#pragma unroll
+        for (int i = 0; i < NB; ++i) v[i] = acc[m][i][j];
+        store_row<float, NB>(to + (wm + (kg * 4 + j) * NB + m) * edge, v, NB, true, false);
+      }
+    return;
+  }
+  E* out = static_cast<E*>(p.out) + (long long)m0 * p.os + n0 + wn + l16 * NB;
+  const int left = p.N - n0 - wn - l16 * NB;
+#pragma unroll
+  for (int m = 0; m < NB; ++m)
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const long long r = m0 + wm + (kg * 4 + j) * 4 + m;
-      if (r >= p.M) continue;
+      const int r = wm + (kg * 4 + j) * NB + m;
+      if (r >= p.M - m0) continue;
+      float v[NB];
 #pragma unroll
-      for (int n = 0; n < 4; ++n) {
-        const long long c = n0 + wn + l16 * 4 + n;
-        if (c < p.N) put_out(out + r * p.os + c, acc[m][n][j], p.accumulate != 0);
-      }
+      for (int i = 0; i < NB; ++i) v[i] = acc[m][i][j];
+      store_row<E, NB>(out + (long long)r * p.os, v, left, p.vec != 0, p.accumulate != 0);
     }
+}
+
+// Adds up the pieces of a split contraction in order.  Four columns per lane, four tile rows per workgroup of 256-wide
+// tiles (eight of 128-wide ones).
+template <int EDGE, typename E> __global__ __launch_bounds__(256) void product_join_kernel(ProductArgs p) {
+  constexpr int rows = 1024 / EDGE, slabs = EDGE / rows;
+  const int tile = blockIdx.x / slabs, r0 = (blockIdx.x - tile * slabs) * rows;
+  const int band = tile / (kTileGroup * p.tiles_n), first = band * kTileGroup;
+  const int high = p.tiles_m - first < kTileGroup ? p.tiles_m - first : kTileGroup;
+  const int in = tile - first * p.tiles_n, tn = in / high, tm = first + in - tn * high;
+  const int r = r0 + threadIdx.x / (EDGE / 4), c = (threadIdx.x % (EDGE / 4)) * 4;
+  if (tm * EDGE + r >= p.M || tn * EDGE + c >= p.N) return;
+  const float* from = p.part + (long long)tile * p.pieces * (EDGE * EDGE) + r * EDGE + c;
+  float v[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int s = 0; s < p.pieces; ++s) {
+    const float4 x = *reinterpret_cast<const float4*>(from + (long long)s * (EDGE * EDGE));
+    v[0] += x.x;
+    v[1] += x.y;
+    v[2] += x.z;
+    v[3] += x.w;
+  }
+  store_row<E, 4>(static_cast<E*>(p.out) + (long long)(tm * EDGE + r) * p.os + tn * EDGE + c, v, p.N - tn * EDGE - c, p.vec != 0,
+                  p.accumulate != 0);
 }
 
 size_t size_of(int dtype) { return is_16bit(dtype) ? 2 : 4; }
@@ -187,9 +400,19 @@ template <typename E, bool FAST> hipError_t launch_pack(const PackArgs& a, unsig
   hipLaunchKernelGGL((pack_blocks_kernel<E, FAST>), dim3(blocks), dim3(256), 0, st, a);
   return hipGetLastError();
 }
-template <typename E> hipError_t launch_product(const ProductArgs& a, unsigned blocks, hipStream_t st) {
-  hipLaunchKernelGGL((product_kernel<E>), dim3(blocks), dim3(256), 0, st, a);
+template <int NB, typename E> hipError_t launch_tiles(const ProductArgs& p, hipStream_t st) {
+  constexpr int lds = TileShape<NB>::lds, edge = TileShape<NB>::edge;
+  auto kern = product_tile_kernel<NB, std::is_same<E, float>::value, E>;
+  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  if (e != hipSuccess) return e;
+  const unsigned total = unsigned(p.tiles_m) * unsigned(p.tiles_n);
+  hipLaunchKernelGGL(kern, dim3((total * p.pieces + kNumXcd - 1) / kNumXcd * kNumXcd), dim3(256), lds, st, p);
+  if (p.part)
+    hipLaunchKernelGGL((product_join_kernel<edge, E>), dim3(total * (edge * edge / 1024)), dim3(256), 0, st, p);
   return hipGetLastError();
+}
+template <typename E> hipError_t launch_product(const ProductArgs& p, int blocks, hipStream_t st) {
+  return blocks == 8 ? launch_tiles<8, E>(p, st) : launch_tiles<4, E>(p, st);
 }
 
 RowSpan values_of(const adloco_blocks8* b) {
@@ -284,8 +507,8 @@ extern "C" int adloco_block_product(adloco_ctx* ctx, const adloco_blocks8* a, co
   for (const adloco_blocks8* x : {a, b})
     if (spans_overlap(so, values_of(x)) || spans_overlap(so, exponents_of(x)))
       return fail(ctx, ADLOCO_EINVAL, "block_product: out overlaps an operand");
-  const int64_t tm = (a->rows + kProductTile - 1) / kProductTile, tn = (b->rows + kProductTile - 1) / kProductTile;
-  if (tm * tn > 0x7fffffffLL) return fail(ctx, ADLOCO_EUNSUPPORTED, "block_product: too many tiles for one launch");
+  if (a->row_stride > (1 << 23) || b->row_stride > (1 << 23))
+    return fail(ctx, ADLOCO_EUNSUPPORTED, "block_product: rows more than 2^23 bytes apart");
   ProductArgs p{};
   p.a = static_cast<const unsigned char*>(a->data);
   p.b = static_cast<const unsigned char*>(b->data);
@@ -300,15 +523,26 @@ extern "C" int adloco_block_product(adloco_ctx* ctx, const adloco_blocks8* a, co
   p.M = int(a->rows);
   p.N = int(b->rows);
   p.steps = int((a->cols + 127) / 128);
-  p.tiles_n = int(tn);
   p.accumulate = flags & ADLOCO_ACCUMULATE ? 1 : 0;
   DeviceScope scope(ctx);
   if (!scope.ok()) return fail(ctx, ADLOCO_EHIP, "block_product: device %d cannot be made current", ctx->device);
   hipStream_t st = static_cast<hipStream_t>(stream);
-  const unsigned n = unsigned(tm * tn);
+  const int blocks = ctx->product_blocks ? ctx->product_blocks : 8;
+  const int64_t edge = 32 * blocks, tm = (a->rows + edge - 1) / edge, tn = (b->rows + edge - 1) / edge;
+  if (tm * tn > 0xffffffLL) return fail(ctx, ADLOCO_EUNSUPPORTED, "block_product: too many tiles for one launch");
+  p.tiles_m = int(tm);
+  p.tiles_n = int(tn);
+  p.pieces = ctx->product_pieces ? ctx->product_pieces : 1;
+  if (p.pieces > p.steps) p.pieces = p.steps;
+  if (p.pieces > 1) {
+    p.part = size_t(tm * tn * p.pieces) * size_t(edge * edge) * sizeof(float) <= kLayerScratch ? layer_scratch(ctx, st) : nullptr;
+    if (!p.part) p.pieces = 1;
+  }
+  const int64_t row = (p.pieces > 1 ? 4 : blocks) * (int64_t)es;
+  p.vec = reinterpret_cast<uintptr_t>(out) % row == 0 && os * (int64_t)es % row == 0;
   hipEvent_t ev = prof_begin(ctx, st);
-  const hipError_t e = dtype == ADLOCO_BF16 ? launch_product<__bf16>(p, n, st)
-                       : dtype == ADLOCO_F16 ? launch_product<_Float16>(p, n, st) : launch_product<float>(p, n, st);
+  const hipError_t e = dtype == ADLOCO_BF16 ? launch_product<__bf16>(p, blocks, st)
+                       : dtype == ADLOCO_F16 ? launch_product<_Float16>(p, blocks, st) : launch_product<float>(p, blocks, st);
   prof_end(ctx, kProfProduct, ev, st);
   if (e != hipSuccess) return fail(ctx, ADLOCO_EHIP, "block_product launch failed: %s", hipGetErrorString(e));
   return ADLOCO_OK;

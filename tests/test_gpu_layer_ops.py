@@ -9,8 +9,11 @@ Tolerances.  u = 2^-24 is the largest relative error of one fp32 operation; half
   blocks        2^-4 of a value (half a step of 3 mantissa bits), 2^-10 of the block's power of two below its normal range.
   backward      w - n mean(w n): 64 + 8 terms again, r, n and the products: (80 u) (|w| + |n| mean|w n|) r, then the sums.
   gain sums     T terms of one sample, in runs: (T + 16) u sum |dy n|, n itself off by 64 u.
-  product       K products, exact, summed in some order with errors of 2 u each (matrix instructions may cut off):
-                2 K u sum |a b|; and exactly where every partial sum is a whole number below 2^24."""
+  product       fp32 output: K products, exact, summed in some order with errors of 2 u each (a matrix instruction may cut
+                off): 2 K u sum |a b|.  16-bit output: the 8-bit instruction cuts every product off below 2^-13 of the
+                largest of a group of at most 32, whose products the bound of 2^-13 * 32 sum |a b| covers; over random
+                values the cuts are independent and their 2-norm is below 2^-13 of that of the products, hence of the
+                sums.  Exactly where every partial sum is a whole number below 2^24 and no product is above 2^6."""
 import numpy as np
 import pytest
 import torch
@@ -201,13 +204,27 @@ PRODUCTS = [(1, 1, 1), (1, 130, 257), (3, 64, 128), (16, 96, 640), (17, 33, 100)
             (2, 3000, 2000), (31, 129, 40000)]
 
 
+# (16 x 16 blocks per wave and side, pieces of the contraction); 0: the library's choice
+VARIANTS = [(0, 0), (4, 1), (8, 1), (4, 3), (8, 2), (4, 7)]
+
+
+@pytest.fixture(params=VARIANTS, ids=lambda v: f"{v[0]}x{v[1]}")
+def variant(ctx, request):
+    ctx.set_tuning("product_blocks", request.param[0])
+    ctx.set_tuning("product_pieces", request.param[1])
+    yield request.param
+    ctx.set_tuning("product_blocks", 0)
+    ctx.set_tuning("product_pieces", 0)
+
+
 @pytest.mark.parametrize("m,n,k", PRODUCTS)
-def test_block_product_of_whole_numbers_is_exact(ctx, m, n, k):
+def test_block_product_of_whole_numbers_is_exact(ctx, variant, m, n, k):
     (a, av), (b, bv) = random_blocks(m + n, m, k, True), random_blocks(k, n, k, True)
     want = av @ bv.T                                   # |partial sums| <= 64 K < 2^24 up to K = 262144
-    out = torch.full((m, n), float("nan"), device=DEV)
-    A.adloco_block_product(ctx, a, b, out)
-    np.testing.assert_array_equal(host(out), want)
+    for dt in TYPES.values():
+        out = torch.full((m, n), float("nan"), dtype=dt, device=DEV)
+        A.adloco_block_product(ctx, a, b, out)
+        assert torch.equal(out.cpu(), torch.from_numpy(want).to(dt))      # the exact sum, rounded once
     base = torch.from_numpy(np.random.default_rng(1).integers(-1000, 1000, (m, n))).float().to(DEV)
     acc = base.clone()
     A.adloco_block_product(ctx, a, b, acc, A.ADLOCO_ACCUMULATE)
@@ -216,18 +233,20 @@ def test_block_product_of_whole_numbers_is_exact(ctx, m, n, k):
 
 @pytest.mark.parametrize("dtype", list(TYPES))
 @pytest.mark.parametrize("m,n,k", [(1, 70, 300), (33, 129, 1000), (129, 260, 513), (300, 300, 4000)])
-def test_block_product(ctx, m, n, k, dtype):
+def test_block_product(ctx, variant, m, n, k, dtype):
     dt = TYPES[dtype]
     (a, av), (b, bv) = random_blocks(m + n, m, k), random_blocks(k, n, k)
-    scale = 2.0**-6 if dtype == "f16" else 1.0         # (within the type's range: 448 * 448 * 2^6 * sqrt(K) is not)
-    if dtype == "f16":
+    if dtype == "f16":                                 # (within the type's range)
         a.exponent[:, :m] -= 9
         b.exponent[:, :n] -= 9
         av, bv = av * 2.0**-9, bv * 2.0**-9
     want, size = av @ bv.T, np.abs(av) @ np.abs(bv).T
     out = torch.full((m, n), float("nan"), dtype=dt, device=DEV)
     A.adloco_block_product(ctx, a, b, out)
-    close(out, want, half(dt) * np.abs(want) + 2 * k * U * size * (1 + half(dt)) + tiny(dt))
+    cut = 2 * k * U if dtype == "f32" else 2.0**-13 * 32 + 2 * k * U
+    close(out, want, half(dt) * np.abs(want) + cut * size * (1 + half(dt)) + tiny(dt))
+    norm = np.linalg.norm(host(out) - want) / np.linalg.norm(want)
+    assert norm < (2e-6 if dtype == "f32" else 2.0**-13 + half(dt)), norm
     again = torch.empty_like(out)
     A.adloco_block_product(ctx, a, b, again)
     assert torch.equal(out, again)                     # a fixed order of summation
@@ -238,7 +257,7 @@ def test_block_product(ctx, m, n, k, dtype):
     assert bool((buf == 7).all())
 
 
-def test_block_product_of_sliced_operands(ctx):
+def test_block_product_of_sliced_operands(ctx, variant):
     (a, av), (b, bv) = random_blocks(1, 96, 640, True), random_blocks(2, 80, 640, True)
     sa = A.Blocks8(a.data[16:], a.exponent[:, 16:], 70, 640)            # rows 16 .. 85
     sb = A.Blocks8(b.data[:, 128:], b.exponent[1:], 80, 500)            # columns 128 .. 627
@@ -249,7 +268,7 @@ def test_block_product_of_sliced_operands(ctx):
     np.testing.assert_array_equal(host(out), av[16:86, 128:628] @ bv[:, 128:628].T)
 
 
-def test_block_product_nan_stays_in_its_row(ctx):
+def test_block_product_nan_stays_in_its_row(ctx, variant):
     (a, av), (b, bv) = random_blocks(3, 200, 300, True), random_blocks(4, 150, 300, True)
     a.data[77, 123] = 0x7F
     b.data[99, 5] = 0xFF
