@@ -63,7 +63,7 @@ struct NormArgs {
 constexpr float kTiny = 1.262177448353619e-29f;   // 2^-96: 16384 squares of the largest fp32 number fit
 
 // Sums over the row of a few values at once; `slot` alternates from row to row, so that one barrier is enough.
-template <int WAVES, int N> __device__ __forceinline__ void row_sums(float (&s)[N], float (*lds)[4][2], int slot) {
+template <int WAVES, int N> __device__ __forceinline__ void row_sums(float (&s)[N], float (*lds)[8][2], int slot) {
 #pragma unroll
   for (int k = 0; k < N; ++k) s[k] = sum64(s[k]);
   if constexpr (WAVES > 1) {
@@ -72,22 +72,33 @@ template <int WAVES, int N> __device__ __forceinline__ void row_sums(float (&s)[
       for (int k = 0; k < N; ++k) lds[slot][threadIdx.x >> 6][k] = s[k];
     __syncthreads();
 #pragma unroll
-    for (int k = 0; k < N; ++k) s[k] = (lds[slot][0][k] + lds[slot][1][k]) + (lds[slot][2][k] + lds[slot][3][k]);
+    for (int k = 0; k < N; ++k) {
+      s[k] = lds[slot][0][k];
+#pragma unroll
+      for (int w = 1; w < WAVES; ++w) s[k] += lds[slot][w][k];
+    }
   }
+}
+// A lane's eight gains of one group; 0 behind the last column.
+__device__ __forceinline__ void load_gain(const float* gain, int c, int d, bool vec, float (&g)[8]) {
+  if (gain && vec && c + 8 <= d) {
+    const float4 a = *reinterpret_cast<const float4*>(gain + c), b = *reinterpret_cast<const float4*>(gain + c + 4);
+    g[0] = a.x; g[1] = a.y; g[2] = a.z; g[3] = a.w;
+    g[4] = b.x; g[5] = b.y; g[6] = b.z; g[7] = b.w;
+    return;
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j) g[j] = c + j >= d ? 0.f : gain ? gain[c + j] : 1.f;
 }
 
 template <typename E, int NV, int WAVES, bool FAST> __global__ __launch_bounds__(64 * WAVES) void rms_norm_kernel(NormArgs a) {
-  __shared__ float lds[4][4][2];
+  __shared__ float lds[4][8][2];
   int slot = 0;
   const int c0 = threadIdx.x * 8;
   float g[NV][8];
+  const bool gain_vec = reinterpret_cast<unsigned long long>(a.gain) % 16 == 0;
 #pragma unroll
-  for (int i = 0; i < NV; ++i)
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int c = c0 + i * 512 * WAVES + j;
-      g[i][j] = c >= a.d ? 0.f : a.gain ? a.gain[c] : 1.f;
-    }
+  for (int i = 0; i < NV; ++i) load_gain(a.gain, c0 + i * 512 * WAVES, a.d, gain_vec, g[i]);
   for (long long row = blockIdx.x; row < a.rows; row += gridDim.x) {
     float h[NV][8], r[NV][8];
 #pragma unroll
@@ -173,27 +184,43 @@ struct NormBackArgs {
 
 template <typename E, int NV, int WAVES, bool FAST>
 __global__ __launch_bounds__(64 * WAVES) void rms_norm_backward_kernel(NormBackArgs a) {
-  __shared__ float lds[4][4][2];
+  __shared__ float lds[4][8][2];
   int slot = 0;
   const int c0 = threadIdx.x * 8;
   const long long sample = blockIdx.x / a.runs;
   const int run = int(blockIdx.x - sample * a.runs);
   const long long first = sample * a.T + a.T * run / a.runs, last = sample * a.T + a.T * (run + 1) / a.runs;
   float acc[NV][8], g[NV][8];
+  const bool gain_vec = reinterpret_cast<unsigned long long>(a.gain) % 16 == 0;
 #pragma unroll
-  for (int i = 0; i < NV; ++i)
+  for (int i = 0; i < NV; ++i) {
+    load_gain(a.gain, c0 + i * 512 * WAVES, a.d, gain_vec, g[i]);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int c = c0 + i * 512 * WAVES + j;
-      acc[i][j] = 0.f;
-      g[i][j] = c >= a.d ? 0.f : a.gain ? a.gain[c] : 1.f;
+    for (int j = 0; j < 8; ++j) acc[i][j] = 0.f;
+  }
+  // the next row is fetched behind the work on this one: two reductions and a store would expose its latency
+  eight<E> rh[NV], ry[NV], ri[NV];
+  auto fetch = [&](long long row) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = c0 + i * 512 * WAVES;
+      rh[i] = fetch_eight<E, FAST>(static_cast<const E*>(a.h) + row * a.hs, c, a.d);
+      ry[i] = fetch_eight<E, FAST>(static_cast<const E*>(a.dy) + row * a.ys, c, a.d);
+      if (a.dh_in) ri[i] = fetch_eight<E, FAST>(static_cast<const E*>(a.dh_in) + row * a.is, c, a.d);
     }
+  };
+  constexpr bool ahead = NV < 4;                    // (wider rows have no registers left for it)
+  if (ahead && first < last) fetch(first);
   for (long long row = first; row < last; ++row) {
-    float h[NV][8], y[NV][8];
+    if (!ahead) fetch(row);
+    float h[NV][8], y[NV][8], in[NV][8];
 #pragma unroll
-    for (int i = 0; i < NV; ++i) load_eight<E, FAST>(static_cast<const E*>(a.h) + row * a.hs, c0 + i * 512 * WAVES, a.d, h[i]);
-#pragma unroll
-    for (int i = 0; i < NV; ++i) load_eight<E, FAST>(static_cast<const E*>(a.dy) + row * a.ys, c0 + i * 512 * WAVES, a.d, y[i]);
+    for (int i = 0; i < NV; ++i) {
+      widen_eight<E>(rh[i], h[i]);
+      widen_eight<E>(ry[i], y[i]);
+      if (a.dh_in) widen_eight<E>(ri[i], in[i]);
+    }
+    if (ahead && row + 1 < last) fetch(row + 1);
     float s[2] = {0.f, 0.f}, eps = a.eps, pre = 1.f;
 #pragma unroll
     for (int i = 0; i < NV; ++i)
@@ -221,14 +248,13 @@ __global__ __launch_bounds__(64 * WAVES) void rms_norm_backward_kernel(NormBackA
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = c0 + i * 512 * WAVES;
-      float v[8], in[8];
-      if (a.dh_in) load_eight<E, FAST>(static_cast<const E*>(a.dh_in) + row * a.is, c, a.d, in);
+      float v[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const float n = h[i][j] * r;
         acc[i][j] = fmaf(y[i][j], n, acc[i][j]);
         v[j] = out * fmaf(-n, mean, g[i][j] * y[i][j]);
-        if (a.dh_in) v[j] += in[j];
+        if (a.dh_in) v[j] += in[i][j];
       }
       if (a.dh) store_eight<E, FAST>(static_cast<E*>(a.dh) + row * a.os, c, a.d, v);
       if (a.dx) {
@@ -247,13 +273,24 @@ __global__ __launch_bounds__(64 * WAVES) void rms_norm_backward_kernel(NormBackA
   }
 }
 
-__global__ __launch_bounds__(64) void gain_runs_kernel(const float* parts, int runs, int d, int slabs, float* out) {
+// Adds up a sample's runs: 64 columns per workgroup, a sixteenth of the runs per wave in order, then the sixteen in order.
+constexpr int kRunWaves = 16;
+__global__ __launch_bounds__(64 * kRunWaves) void gain_runs_kernel(const float* parts, int runs, int d, int slabs, float* out) {
+  __shared__ float lds[kRunWaves][64];
   const long long sample = blockIdx.x / slabs;
-  const int c = int(blockIdx.x - sample * slabs) * 64 + threadIdx.x;
-  if (c >= d) return;
-  const float* p = parts + sample * runs * d + c;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int c = int(blockIdx.x - sample * slabs) * 64 + lane, cc = c < d ? c : d - 1;
+  const float* p = parts + sample * runs * d + cc;
+  const int first = runs * wave / kRunWaves, last = runs * (wave + 1) / kRunWaves;
   float s = 0.f;
-  for (int k = 0; k < runs; ++k) s += p[(long long)k * d];
+#pragma unroll 8
+  for (int k = first; k < last; ++k) s += p[(long long)k * d];
+  lds[wave][lane] = s;
+  __syncthreads();
+  if (wave > 0 || c >= d) return;
+  s = 0.f;
+#pragma unroll
+  for (int k = 0; k < kRunWaves; ++k) s += lds[k][lane];
   out[sample * d + c] = s;
 }
 
@@ -329,21 +366,23 @@ template <typename E, bool FAST> struct LaunchDropout {
   }
 };
 
-// Waves per row and groups of eight columns per lane: one wave holds up to 2048 columns, a workgroup of four the rest.
+// Waves per row and groups of eight columns per lane.  As many waves as the row fills: with 2048 columns on one wave (four
+// groups a lane) the forward pass of 32768 rows takes 118 us, on two 101, on four 99.
 constexpr int kNormWidth = 16384;
+constexpr int norm_waves(int wide) { return wide <= 512 ? 1 : wide <= 1024 ? 2 : wide <= 2048 ? 4 : 8; }
 #define ADLOCO_NORM_SHAPE(wide, CALL)         \
   do {                                        \
     if (wide <= 512) CALL(1, 1);              \
-    else if (wide <= 1024) CALL(2, 1);        \
-    else if (wide <= 2048) CALL(4, 1);        \
-    else if (wide <= 4096) CALL(2, 4);        \
-    else if (wide <= 8192) CALL(4, 4);        \
-    else CALL(8, 4);                          \
+    else if (wide <= 1024) CALL(1, 2);        \
+    else if (wide <= 2048) CALL(1, 4);        \
+    else if (wide <= 4096) CALL(1, 8);        \
+    else if (wide <= 8192) CALL(2, 8);        \
+    else CALL(4, 8);                          \
   } while (0)
 
 template <typename E, bool FAST> struct LaunchNorm {
   static hipError_t run(const NormArgs& a, hipStream_t st) {
-    const long long most = (long long)kNumCu * (a.wide <= 2048 ? 16 : 4);
+    const long long most = (long long)kNumCu * 16 / norm_waves(a.wide);      // sixteen waves per compute unit
     const dim3 grid(unsigned(a.rows < most ? a.rows : most));
 #define ADLOCO_CALL(NV, WAVES) hipLaunchKernelGGL((rms_norm_kernel<E, NV, WAVES, FAST>), grid, dim3(64 * WAVES), 0, st, a)
     ADLOCO_NORM_SHAPE(a.wide, ADLOCO_CALL);
@@ -498,10 +537,12 @@ extern "C" int adloco_rms_norm_backward(adloco_ctx* ctx, const adloco_norm_backw
   DeviceScope scope(ctx);
   if (!scope.ok()) return fail(ctx, ADLOCO_EHIP, "rms_norm_backward: device %d cannot be made current", ctx->device);
   hipStream_t st = static_cast<hipStream_t>(stream);
-  // Runs per sample: enough workgroups to fill the chip, runs of 8 rows at least, their sums within the scratch.
-  const long long wanted = (long long)kNumCu * (d <= 2048 ? 12 : 4);
+  // Runs per sample: enough workgroups to fill the chip, runs of 4 rows at least, their sums within the scratch.  Waves per
+  // compute unit, measured: 32768 x 1024 with dropout 8: 78 us, 16: 70, 20: 74; 32768 x 2048 8: 99, 16: 111; 4096 x 8192 58, 64.
+  const long long least = 4;
+  const long long wanted = (long long)kNumCu * (d <= 1024 ? 16 : 8) / norm_waves(d);
   long long runs = (wanted + B - 1) / B;
-  if (runs > (T + 7) / 8) runs = (T + 7) / 8;
+  if (runs > (T + least - 1) / least) runs = (T + least - 1) / least;
   if (runs < 1) runs = 1;
   float* parts = io->gain_sums;
   if (io->gain_sums && runs > 1) {
@@ -533,7 +574,7 @@ extern "C" int adloco_rms_norm_backward(adloco_ctx* ctx, const adloco_norm_backw
   hipEvent_t ev = prof_begin(ctx, st);
   hipError_t e = by_type<LaunchNormBack>(dtype, fast, a, unsigned(B * runs), st);
   if (e == hipSuccess && io->gain_sums && runs > 1) {
-    hipLaunchKernelGGL(gain_runs_kernel, dim3(unsigned(B * slabs)), dim3(64), 0, st, parts, int(runs), d, slabs, io->gain_sums);
+    hipLaunchKernelGGL(gain_runs_kernel, dim3(unsigned(B * slabs)), dim3(64 * kRunWaves), 0, st, parts, int(runs), d, slabs, io->gain_sums);
     e = hipGetLastError();
   }
   prof_end(ctx, kProfNormBack, ev, st);

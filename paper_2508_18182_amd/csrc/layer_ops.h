@@ -7,31 +7,44 @@ namespace adloco {
 
 // ---- eight consecutive values of a row -----------------------------------------------------------------------------
 // FAST: rows are 16-byte aligned and whole multiples of eight long, so that a lane's eight are all there or all not.
-template <typename E, bool FAST> __device__ __forceinline__ void load_eight(const E* row, int c, int d, float (&v)[8]) {
-  typedef __attribute__((ext_vector_type(8))) E vec;
+// Others are loaded and stored eight at a time all the same, at element alignment; only the last ones of a row go singly
+// (5005 x 771 fp32, residual norm with dropout: 14 us, one by one 39).
+template <typename E> using eight = E __attribute__((ext_vector_type(8)));
+template <typename E, bool FAST> __device__ __forceinline__ eight<E> fetch_eight(const E* row, int c, int d) {
+  eight<E> r = {};
   if constexpr (FAST) {
-    if (c < d) {
-      const vec r = __builtin_nontemporal_load(reinterpret_cast<const vec*>(row + c));
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = float(r[j]);
-      return;
-    }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = 0.f;
+    if (c < d) r = __builtin_nontemporal_load(reinterpret_cast<const eight<E>*>(row + c));
   } else {
+    if (c + 8 <= d) {
+      __builtin_memcpy(&r, row + c, sizeof r);
+    } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = c + j < d ? float(row[c + j]) : 0.f;
+      for (int j = 0; j < 8; ++j)
+        if (c + j < d) r[j] = row[c + j];
+    }
   }
+  return r;
+}
+template <typename E> __device__ __forceinline__ void widen_eight(const eight<E>& r, float (&v)[8]) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = float(r[j]);
+}
+template <typename E, bool FAST> __device__ __forceinline__ void load_eight(const E* row, int c, int d, float (&v)[8]) {
+  widen_eight<E>(fetch_eight<E, FAST>(row, c, d), v);
 }
 template <typename E, bool FAST> __device__ __forceinline__ void store_eight(E* row, int c, int d, const float (&v)[8]) {
-  typedef __attribute__((ext_vector_type(8))) E vec;
   if constexpr (FAST) {
     if (c < d) {
-      vec r;
+      eight<E> r;
 #pragma unroll
       for (int j = 0; j < 8; ++j) r[j] = E(v[j]);
-      __builtin_nontemporal_store(r, reinterpret_cast<vec*>(row + c));
+      __builtin_nontemporal_store(r, reinterpret_cast<eight<E>*>(row + c));
     }
+  } else if (c + 8 <= d) {
+    eight<E> r;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) r[j] = E(v[j]);
+    __builtin_memcpy(row + c, &r, sizeof r);
   } else {
 #pragma unroll
     for (int j = 0; j < 8; ++j)
