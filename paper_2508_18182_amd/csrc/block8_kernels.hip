@@ -22,9 +22,9 @@ const char* check_blocks8(const adloco_blocks8* b) {
 namespace {
 
 // ---------------------------------------------------------------------------------------------------------------------
-// Packing.  A workgroup takes 128 x 128 values, a lane 8 x 8 of them in registers: blocks along the rows are 16 lanes of a
-// row, blocks across them the 16 groups of eight rows.  x is read once whichever of the two outputs are asked for; the
-// transposed one goes through LDS, so that both are stored in whole lines.
+// Packing.  A workgroup of eight waves takes 128 x 128 values, a lane eight columns of four rows in registers: blocks along
+// the rows are 16 lanes of a row, blocks across them the 32 groups of four rows.  x is read once whichever of the two outputs
+// are asked for; the transposed one goes through LDS, so that both are stored in whole lines.
 // ---------------------------------------------------------------------------------------------------------------------
 struct PackArgs {
   const void* x;
@@ -35,67 +35,125 @@ struct PackArgs {
   unsigned col_tiles;
 };
 
-template <typename E, bool FAST> __global__ __launch_bounds__(256) void pack_blocks_kernel(PackArgs a) {
-  __shared__ float big_lds[4][128];
-  __shared__ uint2 turn[128][16];
+constexpr int kPackThreads = 512, kPackRows = 4;
+
+template <typename E, bool FAST> __global__ __launch_bounds__(kPackThreads) void pack_blocks_kernel(PackArgs a) {
+  constexpr int R = kPackRows;
+  __shared__ __attribute__((aligned(16))) unsigned most[128];
+  __shared__ __attribute__((aligned(16))) unsigned turn[128][32];
   const int cg = threadIdx.x & 15, rg = threadIdx.x >> 4;
   const long long rt = blockIdx.x / a.col_tiles, ct = blockIdx.x - rt * a.col_tiles;
-  const long long r0 = rt * 128 + rg * 8, c0 = ct * 128;
+  const long long r0 = rt * 128 + rg * R, c0 = ct * 128;
   const int left = int(a.cols - c0 < 128 ? a.cols - c0 : 128);
-  float v[8][8];
+  if (threadIdx.x < 128) most[threadIdx.x] = 0;
+  // all four rows are requested before the first is looked at (rows and columns behind the last: the last ones again)
+  float v[R][8];
+  {
+    eight<E> raw[R];
+    const int cc = FAST && cg * 8 >= left ? left - 8 : cg * 8;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    if (r0 + i < a.rows) {
-      load_eight<E, FAST>(static_cast<const E*>(a.x) + (r0 + i) * a.xs + c0, cg * 8, left, v[i]);
-    } else {
+    for (int i = 0; i < R; ++i) {
+      const long long r = r0 + i < a.rows ? r0 + i : a.rows - 1;
+      raw[i] = fetch_eight<E, FAST>(static_cast<const E*>(a.x) + r * a.xs + c0, cc, left);
+    }
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
+    for (int i = 0; i < R; ++i) {
+      widen_eight<E>(raw[i], v[i]);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[i][j] = r0 + i < a.rows && cg * 8 + j < left ? v[i][j] : 0.f;
     }
   }
   if (a.q) {
-    unsigned long long exps = 0;
+    unsigned big[R], exps = 0;
+    bool mine = false;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      float big = 0.f;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) big = fmaxf(big, finite_abs(v[i][j]));
-      const unsigned e = block_exponent(max16(big));
-      exps |= (unsigned long long)e << (8 * i);
-      if (r0 + i < a.rows) *reinterpret_cast<uint2*>(a.q + (r0 + i) * a.qs + c0 + cg * 8) = pack_eight(v[i], block_inverse(e));
+    for (int i = 0; i < R; ++i) {
+      big[i] = max16(largest<false>(v[i]));
+      mine = mine || big[i] >= kNotFinite;
     }
-    if (cg == 0) {
-      unsigned char* p = a.e + ct * a.es + r0;
-      if (r0 + 8 <= a.rows) *reinterpret_cast<unsigned long long*>(p) = exps;
-      else
-        for (int i = 0; r0 + i < a.rows; ++i) p[i] = (unsigned char)(exps >> (8 * i));
+    const bool any = __builtin_amdgcn_ballot_w64(mine) != 0;      // (the same for the wave)
+    if (any)
+#pragma unroll
+      for (int i = 0; i < R; ++i) big[i] = max16(largest<true>(v[i]));
+    uint2 out[R];
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      const unsigned e = block_exponent(big[i]);
+      exps |= e << (8 * i);
+      out[i] = pack_eight(v[i], e);
+    }
+    if (any)
+#pragma unroll
+      for (int i = 0; i < R; ++i) mark_eight(v[i], out[i]);
+    unsigned char* q = a.q + r0 * a.qs + c0 + cg * 8;
+    unsigned char* p = a.e + ct * a.es + r0;
+    if (r0 + R <= a.rows) {
+#pragma unroll
+      for (int i = 0; i < R; ++i) *reinterpret_cast<uint2*>(q + i * a.qs) = out[i];
+      if (cg == 0) *reinterpret_cast<unsigned*>(p) = exps;
+    } else {
+#pragma unroll
+      for (int i = 0; i < R; ++i)
+        if (r0 + i < a.rows) {
+          *reinterpret_cast<uint2*>(q + i * a.qs) = out[i];
+          if (cg == 0) p[i] = (unsigned char)(exps >> (8 * i));
+        }
     }
   }
   if (!a.qt) return;
+  // largest magnitude of each column: of a wave's 16 rows by shuffles, of the waves in LDS
+  auto columns = [&](bool finite) {
+    unsigned big[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      big[j] = 0;
+#pragma unroll
+      for (int i = 0; i < R; ++i) big[j] = larger(big[j], finite && magnitude(v[i][j]) >= kNotFinite ? 0u : magnitude(v[i][j]));
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) big[j] = larger(big[j], __shfl_xor(big[j], 16, 64));
+#pragma unroll
+    for (int j = 0; j < 8; ++j) big[j] = larger(big[j], __shfl_xor(big[j], 32, 64));
+    unsigned all = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) all = larger(all, big[j]);
+    if ((threadIdx.x & 63) < 16)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) atomicMax(&most[cg * 8 + j], big[j]);
+    return all >= kNotFinite;
+  };
+  __syncthreads();
+  const bool any = __builtin_amdgcn_readfirstlane(__syncthreads_or(columns(false)));
+  if (any) {                                          // some value of the tile is not finite: the maxima of the others
+    if (threadIdx.x < 128) most[threadIdx.x] = 0;
+    __syncthreads();
+    columns(true);
+    __syncthreads();
+  }
+  const uint4 lo = *reinterpret_cast<const uint4*>(&most[cg * 8]), hi = *reinterpret_cast<const uint4*>(&most[cg * 8 + 4]);
+  const unsigned big[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+  unsigned long long exps = 0;
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    float big = 0.f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) big = fmaxf(big, finite_abs(v[i][j]));
-    big = fmaxf(big, __shfl_xor(big, 16, 64));
-    big = fmaxf(big, __shfl_xor(big, 32, 64));
-    if ((threadIdx.x & 63) < 16) big_lds[threadIdx.x >> 6][cg * 8 + j] = big;
+    const unsigned e = block_exponent(big[j]);
+    unsigned o = pack_four(v[0][j], v[1][j], v[2][j], v[3][j], e);
+    if (any) mark_four(v[0][j], v[1][j], v[2][j], v[3][j], o);
+    // (groups of four words permuted by the column: the lanes of a store spread over the banks)
+    turn[cg * 8 + j][rg ^ ((cg & 7) << 2)] = o;
+    exps |= (unsigned long long)e << (8 * j);
+  }
+  if (rg == 0 && cg * 8 < left) {
+    unsigned char* p = a.et + rt * a.ets + c0 + cg * 8;
+    if (cg * 8 + 8 <= left) *reinterpret_cast<unsigned long long*>(p) = exps;
+    else
+      for (int j = 0; cg * 8 + j < left; ++j) p[j] = (unsigned char)(exps >> (8 * j));
   }
   __syncthreads();
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const int c = cg * 8 + j;
-    const unsigned e = block_exponent(fmaxf(fmaxf(big_lds[0][c], big_lds[1][c]), fmaxf(big_lds[2][c], big_lds[3][c])));
-    float col[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) col[i] = v[i][j];
-    turn[c][rg ^ (c & 15)] = pack_eight(col, block_inverse(e));
-    if (rg == 0 && c0 + c < a.cols) a.et[rt * a.ets + c0 + c] = (unsigned char)e;
-  }
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int c = i * 16 + rg;
-    if (c < left) *reinterpret_cast<uint2*>(a.qt + (c0 + c) * a.qts + rt * 128 + cg * 8) = turn[c][cg ^ (c & 15)];
+  for (int i = 0; i < 2; ++i) {
+    const int c = i * 64 + (threadIdx.x >> 3), q = threadIdx.x & 7;
+    if (c < left)
+      *reinterpret_cast<uint4*>(a.qt + (c0 + c) * a.qts + rt * 128 + q * 16) = *reinterpret_cast<const uint4*>(&turn[c][(q ^ ((c >> 3) & 7)) * 4]);
   }
 }
 
@@ -397,7 +455,7 @@ template <int EDGE, typename E> __global__ __launch_bounds__(256) void product_j
 size_t size_of(int dtype) { return is_16bit(dtype) ? 2 : 4; }
 
 template <typename E, bool FAST> hipError_t launch_pack(const PackArgs& a, unsigned blocks, hipStream_t st) {
-  hipLaunchKernelGGL((pack_blocks_kernel<E, FAST>), dim3(blocks), dim3(256), 0, st, a);
+  hipLaunchKernelGGL((pack_blocks_kernel<E, FAST>), dim3(blocks), dim3(kPackThreads), 0, st, a);
   return hipGetLastError();
 }
 template <int NB, typename E> hipError_t launch_tiles(const ProductArgs& p, hipStream_t st) {

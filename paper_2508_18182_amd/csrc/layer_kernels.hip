@@ -144,15 +144,14 @@ template <typename E, int NV, int WAVES, bool FAST> __global__ __launch_bounds__
       const int c = c0 + i * 512 * WAVES;
       if (a.y) store_eight<E, FAST>(static_cast<E*>(a.y) + row * a.ys, c, a.d, h[i]);
       if (a.q) {
-        float big = 0.f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          h[i][j] = c + j < a.d ? h[i][j] : 0.f;     // (in a row whose norm is not finite, 0 * NaN)
-          big = fmaxf(big, finite_abs(h[i][j]));
-        }
-        const unsigned e = block_exponent(max16(big));
+        for (int j = 0; j < 8; ++j) h[i][j] = c + j < a.d ? h[i][j] : 0.f;       // (in a row whose norm is not finite, 0 * NaN)
+        bool any;
+        const unsigned e = row_block(h[i], any);
         if (c < a.wide) {
-          *reinterpret_cast<uint2*>(a.q + row * a.qs + c) = pack_eight(h[i], block_inverse(e));
+          uint2 o = pack_eight(h[i], e);
+          if (any) mark_eight(h[i], o);
+          *reinterpret_cast<uint2*>(a.q + row * a.qs + c) = o;
           if ((threadIdx.x & 15) == 0) a.e[(long long)(c >> 7) * a.es + row] = (unsigned char)e;
         }
       }

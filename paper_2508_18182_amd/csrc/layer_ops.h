@@ -87,47 +87,68 @@ __device__ __forceinline__ void drop_eight(const DropoutArgs& m, long long row, 
 }
 
 // ---- 8-bit blocks --------------------------------------------------------------------------------------------------
-// |x|, or 0 where x is not finite (those become NaN below and have no say in the block's exponent).
-__device__ __forceinline__ float finite_abs(float x) {
-  const float a = fabsf(x);
-  return a <= 3.402823466e38f ? a : 0.f;
+// Magnitudes are compared as bits: their order is that of the numbers, with infinities and NaN above them all, so that one
+// maximum serves both the exponent and the question whether a block holds any of those.
+constexpr unsigned kNotFinite = 0x7f800000u;
+__device__ __forceinline__ unsigned magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+__device__ __forceinline__ unsigned larger(unsigned a, unsigned b) { return a > b ? a : b; }
+// Largest magnitude of eight values; FINITE: infinities and NaN, which have no say in a block's exponent, left out.
+template <bool FINITE> __device__ __forceinline__ unsigned largest(const float (&v)[8]) {
+  unsigned big = 0;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const unsigned m = magnitude(v[j]);
+    big = larger(big, FINITE && m >= kNotFinite ? 0u : m);
+  }
+  return big;
 }
-// Biased exponent of the smallest power of two s >= 2^-126 with big <= 448 s, 448 = 1.75 * 2^8 the largest e4m3 value: read
-// off the bits of `big`, hence exact.
-__device__ __forceinline__ unsigned block_exponent(float big) {
-  const unsigned b = __float_as_uint(big);
-  const int e = int(b >> 23) - 8 + ((b & 0x7fffffu) > 0x600000u ? 1 : 0);
+// Biased exponent of the smallest power of two s >= 2^-126 with x <= 448 s for the finite magnitude x of these bits,
+// 448 = 1.75 * 2^8 the largest e4m3 value: read off the bits, hence exact.
+__device__ __forceinline__ unsigned block_exponent(unsigned big) {
+  const int e = int(big >> 23) - 8 + ((big & 0x7fffffu) > 0x600000u ? 1 : 0);
   return unsigned(e < 1 ? 1 : e);
 }
-__device__ __forceinline__ float block_inverse(unsigned exponent) { return __uint_as_float((254u - exponent) << 23); }
-// Eight values times `inv` (a power of two, hence exact) to e4m3, round to nearest even: at most half a step, 2^-4 of a
-// value that is not below 2^-6.  The largest is 448 by the choice of the exponent, so that nothing saturates.
-__device__ __forceinline__ uint2 pack_eight(const float (&v)[8], float inv) {
-  uint2 out;
-  unsigned* o = &out.x;
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    int w = 0;
-    w = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * h] * inv, v[4 * h + 1] * inv, w, false);
-    w = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * h + 2] * inv, v[4 * h + 3] * inv, w, true);
-    unsigned u = unsigned(w);
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (!(fabsf(v[4 * h + j]) <= 3.402823466e38f)) u |= 0x7fu << (8 * j);     // infinities too: e4m3 has none
-    o[h] = u;
-  }
-  return out;
+// Four values over the block's power of two (exact) to e4m3, round to nearest even: at most half a step, 2^-4 of a value
+// that is not below 2^-6.  The largest is 448 by the choice of the exponent, so that nothing saturates.
+__device__ __forceinline__ unsigned pack_four(float a, float b, float c, float d, unsigned exponent) {
+  typedef __attribute__((ext_vector_type(2))) short i16x2;
+  const float s = __uint_as_float(exponent << 23);
+  i16x2 w = {0, 0};
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, a, b, s, false);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, c, d, s, true);
+  return __builtin_bit_cast(unsigned, w);
 }
-// Maximum over groups of 16 lanes, in all of them.  Every lane of the wave has to be there.
-__device__ __forceinline__ float max16(float v) {
-#define ADLOCO_ROR_MAX(n) \
-  v = fmaxf(v, __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), 0x120 + n, 0xf, 0xf, false)))
+// Values that are not finite become NaN (e4m3 has no infinity).
+__device__ __forceinline__ void mark_four(float a, float b, float c, float d, unsigned& o) {
+  if (magnitude(a) >= kNotFinite) o |= 0x7fu;
+  if (magnitude(b) >= kNotFinite) o |= 0x7f00u;
+  if (magnitude(c) >= kNotFinite) o |= 0x7f0000u;
+  if (magnitude(d) >= kNotFinite) o |= 0x7f000000u;
+}
+__device__ __forceinline__ uint2 pack_eight(const float (&v)[8], unsigned exponent) {
+  return make_uint2(pack_four(v[0], v[1], v[2], v[3], exponent), pack_four(v[4], v[5], v[6], v[7], exponent));
+}
+__device__ __forceinline__ void mark_eight(const float (&v)[8], uint2& o) {
+  mark_four(v[0], v[1], v[2], v[3], o.x);
+  mark_four(v[4], v[5], v[6], v[7], o.y);
+}
+// Maximum over groups of 16 lanes, in all of them.  All lanes of a group have to be there.
+__device__ __forceinline__ unsigned max16(unsigned v) {
+#define ADLOCO_ROR_MAX(n) v = larger(v, unsigned(__builtin_amdgcn_update_dpp(0, int(v), 0x120 + n, 0xf, 0xf, false)))
   ADLOCO_ROR_MAX(8);
   ADLOCO_ROR_MAX(4);
   ADLOCO_ROR_MAX(2);
   ADLOCO_ROR_MAX(1);
 #undef ADLOCO_ROR_MAX
   return v;
+}
+// Biased exponent of the block that 16 lanes hold eight values each of.  any (the same for the wave): some value of the wave
+// is not finite.
+__device__ __forceinline__ unsigned row_block(const float (&v)[8], bool& any) {
+  unsigned big = max16(largest<false>(v));
+  any = __builtin_amdgcn_ballot_w64(big >= kNotFinite) != 0;
+  if (any) big = max16(largest<true>(v));
+  return block_exponent(big);
 }
 __device__ __forceinline__ float sum64(float v) {
 #define ADLOCO_ROR_ADD(n) \
