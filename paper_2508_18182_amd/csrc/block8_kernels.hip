@@ -1,6 +1,7 @@
 // 8-bit blocks: packing of a matrix along its rows and / or across them, and the product of two packed matrices on the
 // scaled matrix instructions.
 #include <type_traits>
+#include <utility>
 
 #include "layer_ops.h"
 
@@ -169,11 +170,13 @@ template <typename E, bool FAST> __global__ __launch_bounds__(kPackThreads) void
 // Which 32 of the 128 values of k a lane holds does not matter as long as both operands agree; which 16 rows make a block of
 // the tile is free too, and a lane takes neighbouring rows for the blocks (row = lane * NB + block), so that their exponents
 // are one load and a lane's outputs of a row one store.
-//   A workgroup of four waves forms a tile of 2 x 2 wave tiles of (16 NB)^2.  Blocks of k come by direct loads into one of two
-// LDS stages (rows of 128 bytes, 16-byte chunks permuted so that eight neighbouring rows lie in different banks).  Per
-// block: the rows of A stream through a few registers, those of B are held; once the last row of A has been read, the
-// workgroup meets, the stage just read takes the block after next, and the rows of B of the next block are fetched behind the
-// last products of this one.
+//   A workgroup of four waves forms a tile of 2 x 2 wave tiles of 16 MB x 16 NB.  Blocks of k come by direct loads into one of
+// two LDS stages (rows of 128 bytes, 16-byte chunks permuted so that eight neighbouring rows lie in different banks).  Per
+// block, the rows of B are held in registers and those of A stream through a few.  What bounds it is the way from L2 to LDS
+// (31 to 39 bytes per clock and compute unit; a 256 x 256 tile needs 32 at the full rate of the matrix cores), so that loads
+// have to be under way all the time: the workgroup meets twice per block and refills in two parts whatever has been read --
+// after the first half of A's blocks their place and B's, after the second half theirs -- which gives every load one and a
+// half blocks of time until it is needed, out of two stages.
 // ---------------------------------------------------------------------------------------------------------------------
 typedef __attribute__((ext_vector_type(8))) int mfma_i32x8;
 typedef __attribute__((ext_vector_type(4))) int i32x4;
@@ -186,11 +189,18 @@ struct ProductArgs {
   long long os;
   int M, N, steps;             // steps: blocks of k
   int tiles_m, tiles_n, pieces;
-  int accumulate, vec;         // vec: NB outputs of a row are one aligned store
+  int accumulate, vec;         // vec: a lane's outputs of a row are one aligned store
 };
 
 constexpr int kTileGroup = 4;  // tile rows that an XCD walks down before it takes the next tile column
 
+__device__ __forceinline__ void tile_place(const ProductArgs& p, int tile, int& tm, int& tn) {
+  const int band = tile / (kTileGroup * p.tiles_n), first = band * kTileGroup;
+  const int high = p.tiles_m - first < kTileGroup ? p.tiles_m - first : kTileGroup;
+  const int in = tile - first * p.tiles_n;
+  tn = in / high;
+  tm = first + in - tn * high;
+}
 // Tile and piece of a workgroup: consecutive workgroups go to the eight XCDs in turn, each XCD gets a contiguous run of the
 // tiles, in bands of kTileGroup tile rows, so that what shares an L2 shares rows of A and columns of B.
 __device__ __forceinline__ bool product_place(const ProductArgs& p, int& tm, int& tn, int& piece, int& tile) {
@@ -199,11 +209,7 @@ __device__ __forceinline__ bool product_place(const ProductArgs& p, int& tm, int
   if (int(blockIdx.x / kNumXcd) >= per || w >= total) return false;
   tile = w / p.pieces;
   piece = w - tile * p.pieces;
-  const int band = tile / (kTileGroup * p.tiles_n), first = band * kTileGroup;
-  const int high = p.tiles_m - first < kTileGroup ? p.tiles_m - first : kTileGroup;
-  const int in = tile - first * p.tiles_n;
-  tn = in / high;
-  tm = first + in - tn * high;
+  tile_place(p, tile, tm, tn);
   return true;
 }
 
@@ -241,17 +247,6 @@ __device__ __forceinline__ void scaled_mfma(mfma_f32x4& c, const mfma_i32x8& a, 
   else
     c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, SEL_A, ea, SEL_B, eb);
 }
-template <int SEL_A, int NB>
-__device__ __forceinline__ void scaled_row(mfma_f32x4 (&c)[NB], const mfma_i32x8& a, const mfma_i32x8 (&b)[NB], int ea, const int (&eb)[NB / 4]) {
-#pragma unroll
-  for (int n = 0; n < NB; n += 4) {
-    scaled_mfma<SEL_A, 0, NB == 8>(c[n], a, b[n], ea, eb[n / 4]);
-    scaled_mfma<SEL_A, 1, NB == 8>(c[n + 1], a, b[n + 1], ea, eb[n / 4]);
-    scaled_mfma<SEL_A, 2, NB == 8>(c[n + 2], a, b[n + 2], ea, eb[n / 4]);
-    scaled_mfma<SEL_A, 3, NB == 8>(c[n + 3], a, b[n + 3], ea, eb[n / 4]);
-  }
-}
-
 template <typename E, int NB> __device__ __forceinline__ void store_row(E* p, const float (&v)[NB], int left, bool vec, bool accumulate) {
   typedef __attribute__((ext_vector_type(NB))) E row;
   if (vec && left >= NB) {
@@ -274,181 +269,244 @@ template <typename E, int NB> __device__ __forceinline__ void store_row(E* p, co
     }
 }
 
-template <int NB> struct TileShape {
-  static constexpr int wave = 16 * NB, edge = 2 * wave;
-  static constexpr int stage = 2 * edge * 128 + 2 * edge;      // A, B, their exponents
+template <int MB, int NB, bool EXACT> struct TileShape {
+  static constexpr int wave_m = 16 * MB, wave_n = 16 * NB, edge_m = 2 * wave_m, edge_n = 2 * wave_n, rows = edge_m + edge_n;
+  static constexpr int stage = rows * 128 + rows;              // values of A, of B; exponents of A, of B
   static constexpr int lds = 2 * stage;
-  static constexpr int resident = NB == 8 ? 1 : 2;             // workgroups per compute unit
+  static constexpr int resident = MB * NB == 16 ? 2 : 1;       // workgroups per compute unit
+  static constexpr int ahead = MB == 8 ? 3 : 1;                // rows of A fetched before they are multiplied
+  static constexpr int first_loads = MB / 2 + NB + 1, second_loads = MB / 2;   // direct loads per wave: B, exponents and the
+                                                                               // first half of A; the second half
 };
 
-template <int NB, bool EXACT, typename E>
-__global__ __launch_bounds__(256, TileShape<NB>::resident) void product_tile_kernel(ProductArgs p) {
-  constexpr int edge = TileShape<NB>::edge, wave_edge = TileShape<NB>::wave, stage = TileShape<NB>::stage;
+template <int N> __device__ __forceinline__ void product_wait() {
+  static_assert(N < 64, "the counter has six bits");
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
+}
+
+template <typename F, int... K> __device__ __forceinline__ void for_each_index(F& f, std::integer_sequence<int, K...>) {
+  (f(std::integral_constant<int, K>{}), ...);
+}
+
+template <int MB, int NB, bool EXACT, typename E>
+__global__ __launch_bounds__(256, (TileShape<MB, NB, EXACT>::resident)) void product_tile_kernel(ProductArgs p) {
+  using T = TileShape<MB, NB, EXACT>;
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
   int tm, tn, piece, tile;
   if (!product_place(p, tm, tn, piece, tile)) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l16 = lane & 15, kg = lane >> 4;
-  const int m0 = tm * edge, n0 = tn * edge;
-  const int s0 = int((long long)p.steps * piece / p.pieces), s1 = int((long long)p.steps * (piece + 1) / p.pieces);
+  const int m0 = tm * T::edge_m, n0 = tn * T::edge_n;
+  const int s0 = int((long long)p.steps * piece / p.pieces), n_steps = int((long long)p.steps * (piece + 1) / p.pieces) - s0;
   const unsigned at = lds_address(lds);
 
-  // Direct loads: a wave brings NB times eight rows of each operand.  Slot q of a stage holds row (q % 16) * NB + q / 16 of
-  // its wave tile (the 16 rows of a block side by side), chunk c of it at place c ^ (q % 8).
-  const int slot = wave * NB * 8 + (lane >> 3), chunk = ((lane & 7) ^ (lane >> 3)) * 16;
-  const int last_a = p.M - m0 - 1, last_b = p.N - n0 - 1;
-  auto row_offset = [&](int i, int last, int stride) {         // (rows behind the last one: the last one again)
-    const int q = slot + i * 8, in = q % wave_edge, r = q - in + (in & 15) * NB + (in >> 4);
-    return __umul24(unsigned(r < last ? r : last), unsigned(stride)) + chunk;
+  // Direct loads of eight rows each.  Slot q of a wave tile holds its row (q % 16) * MB + q / 16 (the 16 rows of a block side
+  // by side), chunk c of it at place c ^ (q / 2 % 8): the 16 lanes of a read
+  // that go together lie in all 64 banks.  Rows behind the last one are the last one again.
+  const int chunk = ((lane & 7) ^ (lane >> 4)) * 16, last_a = p.M - m0 - 1, last_b = p.N - n0 - 1;
+  auto offset = [&](int tile_row, int q, int blocks, int last, long long stride) {
+    const int in = q + (lane >> 3), r = tile_row + (in & 15) * blocks + (in >> 4);
+    return __umul24(unsigned(r < last ? r : last), unsigned(stride)) + (chunk ^ ((q & 8) * 8));
   };
+  // A: load i of MB brings blocks of half i / (MB / 2) of both wave tiles' rows
+  auto slot_a = [&](int i, int& t) {
+    const int u = wave * (MB / 2) + i % (MB / 2);
+    t = u / MB;
+    return i / (MB / 2) * 8 * MB + (u % MB) * 8;
+  };
+  auto slot_b = [&](int i, int& t) {
+    const int u = wave * NB + i;
+    t = u / (2 * NB);
+    return (u % (2 * NB)) * 8;
+  };
+  unsigned off_a[MB], off_b[NB];
+#pragma unroll
+  for (int i = 0; i < MB; ++i) {
+    int t;
+    const int q = slot_a(i, t);
+    off_a[i] = offset(t * T::wave_m, q, MB, last_a, p.as);
+  }
+#pragma unroll
+  for (int i = 0; i < NB; ++i) {
+    int t;
+    const int q = slot_b(i, t);
+    off_b[i] = offset(t * T::wave_n, q, NB, last_b, p.bs);
+  }
   const unsigned char* base_a = uniform_ptr(p.a + (long long)m0 * p.as + (long long)s0 * 128);
   const unsigned char* base_b = uniform_ptr(p.b + (long long)n0 * p.bs + (long long)s0 * 128);
-  // exponents, four rows a lane: wave 0 those of A and wave 1 those of B, or wave 0 both where 32 lanes are enough for each
-  const bool of_b = NB == 8 ? wave == 1 : lane >= 32;
-  const int er = (NB == 8 ? lane : lane & 31) * 4, rows = of_b ? p.N - n0 : p.M - m0;
-  const unsigned char* pe = (of_b ? p.eb + (long long)s0 * p.ebs + n0 : p.ea + (long long)s0 * p.eas + m0) + (er < rows ? er : 0);
-  const long long pe_step = of_b ? p.ebs : p.eas;
-  auto load = [&](int buf) {
-    const unsigned to = at + buf * stage + wave * (NB * 1024);
-#pragma unroll
-    for (int i = 0; i < NB; ++i) direct_load_lds16_s(row_offset(i, last_a, int(p.as)), base_a, to + i * 1024);
-#pragma unroll
-    for (int i = 0; i < NB; ++i) direct_load_lds16_s(row_offset(i, last_b, int(p.bs)), base_b, to + edge * 128 + i * 1024);
-    if (wave < (NB == 8 ? 2 : 1)) direct_load_lds4(pe, at + buf * stage + 2 * edge * 128 + (NB == 8 && wave == 1 ? edge : 0));
-    base_a += 128;
-    base_b += 128;
-    pe += pe_step;
+  auto load_a = [&](int buf, int i) {
+    int t;
+    const int q = slot_a(i, t);
+    direct_load_lds16_s(off_a[i], base_a, at + buf * T::stage + (t * T::wave_m + q) * 128);
   };
-  auto meet = [&] {            // everything asked for is here, for all waves
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+  auto load_b = [&](int buf, int i) {
+    int t;
+    const int q = slot_b(i, t);
+    direct_load_lds16_s(off_b[i], base_b, at + buf * T::stage + (T::edge_m + t * T::wave_n + q) * 128);
+  };
+  // exponents, four rows a lane; a wave brings 256 bytes of A's and B's (the four waves all of them, some twice)
+  const int e_at = (wave & 1) * (T::rows - 256) + lane * 4;
+  const bool of_b = e_at >= T::edge_m;
+  const int e_row = of_b ? e_at - T::edge_m : e_at, e_rows = of_b ? p.N - n0 : p.M - m0;
+  const unsigned char* pe = (of_b ? p.eb + (long long)s0 * p.ebs + n0 : p.ea + (long long)s0 * p.eas + m0) + (e_row < e_rows ? e_row : 0);
+  const long long pe_step = of_b ? p.ebs : p.eas;
+  int loaded = 0;
+  auto load_first = [&](int buf, int i) {             // item i of first_loads
+    if (i == 0) {
+      direct_load_lds4(pe, at + buf * T::stage + T::rows * 128 + (wave & 1) * (T::rows - 256));
+    } else if (i <= NB) {
+      load_b(buf, i - 1);
+    } else {
+      load_a(buf, i - 1 - NB);
+    }
+  };
+  auto load_second = [&](int buf, int i) {
+    load_a(buf, MB / 2 + i);
+    if (i == MB / 2 - 1 && ++loaded < n_steps) {      // to the next block; behind the last one, that one again
+      base_a += 128;
+      base_b += 128;
+      pe += pe_step;
+    }
+  };
+  auto meet = [&] {
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
   };
-  const int wm = (wave >> 1) * wave_edge, wn = (wave & 1) * wave_edge;
-  const int key = l16 & 7;
-  const int row_a = (wm + l16) * 128, row_b = edge * 128 + (wn + l16) * 128;
+  const int wm = (wave >> 1) * T::wave_m, wn = (wave & 1) * T::wave_n;
+  const int key = l16 >> 1;
+  const int row_a = (wm + l16) * 128, row_b = (T::edge_m + wn + l16) * 128;
   const int c0 = ((kg * 2) ^ key) * 16, c1 = ((kg * 2 + 1) ^ key) * 16;
   auto frag = [&](int buf, int row, int block) {
-    const unsigned char* q = lds + buf * stage + row + block * 2048;
+    const unsigned char* q = lds + buf * T::stage + row + block * 2048;
     const i32x4 x = *reinterpret_cast<const i32x4*>(q + c0), y = *reinterpret_cast<const i32x4*>(q + c1);
     return mfma_i32x8{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
   };
-  struct Exps { int a[NB / 4], b[NB / 4]; };
-  auto exps = [&](int buf, Exps& e) {
-    const unsigned char* q = lds + buf * stage + 2 * edge * 128;
+
+  constexpr bool pinned = MB * NB == 64 && !EXACT;
+  constexpr int ahead = T::ahead;
+  mfma_f32x4 acc[MB][NB] = {};
+  if constexpr (pinned) mfma_fence(acc);
+  struct Held { mfma_i32x8 b[NB], a[ahead]; int ea[MB / 4], eb[NB / 4]; };
+  constexpr int fetches = 1 + ahead + NB;
+  auto fetch = [&](int buf, Held& h, int i) {         // item i of fetches
+    const unsigned char* q = lds + buf * T::stage + T::rows * 128;
+    if (i == 0) {
 #pragma unroll
-    for (int i = 0; i < NB / 4; ++i) {
-      e.a[i] = *reinterpret_cast<const int*>(q + wm + l16 * NB + i * 4);
-      e.b[i] = *reinterpret_cast<const int*>(q + edge + wn + l16 * NB + i * 4);
+      for (int x = 0; x < MB / 4; ++x) h.ea[x] = *reinterpret_cast<const int*>(q + wm + l16 * MB + x * 4);
+#pragma unroll
+      for (int x = 0; x < NB / 4; ++x) h.eb[x] = *reinterpret_cast<const int*>(q + T::edge_m + wn + l16 * NB + x * 4);
+    } else if (i == 1) {
+      h.a[0] = frag(buf, row_a, 0);
+    } else if (i < 2 + NB) {
+      h.b[i - 2] = frag(buf, row_b, i - 2);
+    } else {
+      h.a[i - 1 - NB] = frag(buf, row_a, i - 1 - NB);
     }
   };
-
-  constexpr bool pinned = NB == 8 && !EXACT;
-  mfma_f32x4 acc[NB][NB] = {};
-  if constexpr (pinned) mfma_fence(acc);
-  struct Held { mfma_i32x8 b[NB], a0, a1; Exps e; };
-  constexpr int ahead = 2;                            // rows of A fetched before they are multiplied
-  auto fetch = [&](int buf, Held& h) {
-    exps(buf, h.e);
+  // Block s of the piece, in stage s % 2.  Loads are asked for in the order first(s), second(s), first(s + 1), ..; two blocks
+  // are under way at most, and a wait leaves those behind the one it is for.  Blocks behind the last one are loaded and
+  // fetched like any other (the last one again, into places that nobody reads any more), so that all steps are alike.
+  // A wave issues in order, and a matrix instruction keeps the matrix core busy for eight issue slots: loads and LDS reads are
+  // dealt out one by one between them.
+  auto step = [&](int buf, Held& h, Held& next) {
+    constexpr int meet_1 = (MB / 2 - ahead) * NB, meet_2 = (MB - ahead) * NB, end = MB * NB;
+    mfma_i32x8 a[MB];
 #pragma unroll
-    for (int n = 0; n < NB; ++n) h.b[n] = frag(buf, row_b, n);
-    h.a0 = frag(buf, row_a, 0);
-    h.a1 = frag(buf, row_a, 1);
-  };
-  auto step = [&](int buf, bool more, bool load_next, Held& h, Held& next) {
-    mfma_i32x8 a[NB];
-    a[0] = h.a0;
-    a[1] = h.a1;
-    WideFrag wb[EXACT ? NB : 1];
-    if constexpr (EXACT)
-#pragma unroll
-      for (int n = 0; n < NB; ++n) wb[n] = widen(h.b[n], (unsigned(h.e.b[n / 4]) >> (8 * (n & 3))) & 255u);
-#pragma unroll
-    for (int m = 0; m < NB; ++m) {
-      if (m + ahead < NB) a[m + ahead] = frag(buf, row_a, m + ahead);
-      if (m == NB - ahead) {                          // the stage has been read by this wave
-        if (more) {
-          meet();
-          if (load_next) load(buf);
-          fetch(buf ^ 1, next);
-        }
+    for (int i = 0; i < ahead; ++i) a[i] = h.a[i];
+    WideFrag wa, wb[EXACT ? NB : 1];
+    auto slot = [&](auto index) {
+      constexpr int k = decltype(index)::value, m = k / NB, n = k % NB;
+      if constexpr (k == meet_1) {                    // B and the first half of A have been read; the second half is needed
+        product_wait<T::first_loads + T::second_loads>();
+        meet();
+      }
+      if constexpr (k == meet_2) {                    // all of A has been read; the next block's first part is needed
+        product_wait<T::first_loads + T::second_loads>();
+        meet();
       }
       if constexpr (EXACT) {
-        const WideFrag wa = widen(a[m], (unsigned(h.e.a[m / 4]) >> (8 * (m & 3))) & 255u);
+        if (n == 0) wa = widen(a[m], (unsigned(h.ea[m / 4]) >> (8 * (m & 3))) & 255u);
+        if (m == 0) wb[n] = widen(h.b[n], (unsigned(h.eb[n / 4]) >> (8 * (n & 3))) & 255u);
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-#pragma unroll
-          for (int n = 0; n < NB; ++n) acc[m][n] = mfma_16x16x32_v<false>(wa.k[k], wb[n].k[k], acc[m][n]);
+        for (int x = 0; x < 4; ++x) acc[m][n] = mfma_16x16x32_v<false>(wa.k[x], wb[n].k[x], acc[m][n]);
       } else {
-        if (m % 4 == 0) scaled_row<0, NB>(acc[m], a[m], h.b, h.e.a[m / 4], h.e.b);
-        if (m % 4 == 1) scaled_row<1, NB>(acc[m], a[m], h.b, h.e.a[m / 4], h.e.b);
-        if (m % 4 == 2) scaled_row<2, NB>(acc[m], a[m], h.b, h.e.a[m / 4], h.e.b);
-        if (m % 4 == 3) scaled_row<3, NB>(acc[m], a[m], h.b, h.e.a[m / 4], h.e.b);
+        scaled_mfma<(m & 3), (n & 3), pinned>(acc[m][n], a[m], h.b[n], h.ea[m / 4], h.eb[n / 4]);
+      }
+      if constexpr (n == 0 && m + ahead < MB) a[m + ahead] = frag(buf, row_a, m + ahead);
+      if constexpr (k >= meet_1 && k < meet_2) {
+#pragma unroll
+        for (int i = 0; i < T::first_loads; ++i)
+          if (k == meet_1 + i * (meet_2 - meet_1) / T::first_loads) load_first(buf, i);
+      }
+      if constexpr (k >= meet_2) {
+#pragma unroll
+        for (int i = 0; i < fetches; ++i)
+          if (k == meet_2 + i * (end - meet_2) / fetches) fetch(buf ^ 1, next, i);
+#pragma unroll
+        for (int i = 0; i < T::second_loads; ++i)
+          if (k == meet_2 + (2 * i + 1) * (end - meet_2) / (2 * T::second_loads)) load_second(buf, i);
       }
       __builtin_amdgcn_sched_barrier(0);
-    }
+    };
+    for_each_index(slot, std::make_integer_sequence<int, end>{});
+  };
+  auto load = [&](int buf) {
+#pragma unroll
+    for (int i = 0; i < T::first_loads; ++i) load_first(buf, i);
+#pragma unroll
+    for (int i = 0; i < T::second_loads; ++i) load_second(buf, i);
   };
   load(0);
+  load(1);
+  product_wait<T::first_loads + 2 * T::second_loads>();
   meet();
-  const int n = s1 - s0;                              // >= 1
-  if (n > 1) load(1);
   Held h0, h1;
-  fetch(0, h0);
-  for (int s = 0; s < n; s += 2) {
-    step(0, s + 1 < n, s + 2 < n, h0, h1);
-    if (s + 1 < n) step(1, s + 2 < n, s + 3 < n, h1, h0);
+#pragma unroll
+  for (int i = 0; i < fetches; ++i) fetch(0, h0, i);
+  for (int s = 0; s + 1 < n_steps; s += 2) {
+    step(0, h0, h1);
+    step(1, h1, h0);
   }
+  if (n_steps & 1) step(0, h0, h1);
 
   if constexpr (pinned) mfma_fence(acc);
-  // element j of block (m, n): row (kg * 4 + j) * NB + m of the wave tile, column l16 * NB + n
-  if (p.part) {
-    float* to = p.part + ((long long)tile * p.pieces + piece) * (edge * edge) + wn + l16 * NB;
-#pragma unroll
-    for (int m = 0; m < NB; ++m)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        float v[NB];
-#pragma unroll
-        for (int i = 0; i < NB; ++i) v[i] = acc[m][i][j];
-        store_row<float, NB>(to + (wm + (kg * 4 + j) * NB + m) * edge, v, NB, true, false);
-      }
-    return;
-  }
-  E* out = static_cast<E*>(p.out) + (long long)m0 * p.os + n0 + wn + l16 * NB;
+  // element j of block (m, n): row (kg * 4 + j) * MB + m of the wave tile, column l16 * NB + n
+  float* const part = p.part ? p.part + ((long long)tile * p.pieces + piece) * (T::edge_m * T::edge_n) + wn + l16 * NB : nullptr;
+  E* const out = static_cast<E*>(p.out) + (long long)m0 * p.os + n0 + wn + l16 * NB;
   const int left = p.N - n0 - wn - l16 * NB;
 #pragma unroll
-  for (int m = 0; m < NB; ++m)
+  for (int m = 0; m < MB; ++m)
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const int r = wm + (kg * 4 + j) * NB + m;
-      if (r >= p.M - m0) continue;
+      const int r = wm + (kg * 4 + j) * MB + m;
       float v[NB];
 #pragma unroll
       for (int i = 0; i < NB; ++i) v[i] = acc[m][i][j];
-      store_row<E, NB>(out + (long long)r * p.os, v, left, p.vec != 0, p.accumulate != 0);
+      if (part) store_row<float, NB>(part + r * T::edge_n, v, NB, true, false);
+      else if (r < p.M - m0) store_row<E, NB>(out + (long long)r * p.os, v, left, p.vec != 0, p.accumulate != 0);
     }
+  product_wait<0>();                                  // no load may reach LDS that is another workgroup's by then
 }
 
-// Adds up the pieces of a split contraction in order.  Four columns per lane, four tile rows per workgroup of 256-wide
-// tiles (eight of 128-wide ones).
-template <int EDGE, typename E> __global__ __launch_bounds__(256) void product_join_kernel(ProductArgs p) {
-  constexpr int rows = 1024 / EDGE, slabs = EDGE / rows;
-  const int tile = blockIdx.x / slabs, r0 = (blockIdx.x - tile * slabs) * rows;
-  const int band = tile / (kTileGroup * p.tiles_n), first = band * kTileGroup;
-  const int high = p.tiles_m - first < kTileGroup ? p.tiles_m - first : kTileGroup;
-  const int in = tile - first * p.tiles_n, tn = in / high, tm = first + in - tn * high;
-  const int r = r0 + threadIdx.x / (EDGE / 4), c = (threadIdx.x % (EDGE / 4)) * 4;
-  if (tm * EDGE + r >= p.M || tn * EDGE + c >= p.N) return;
-  const float* from = p.part + (long long)tile * p.pieces * (EDGE * EDGE) + r * EDGE + c;
+// Adds up the pieces of a split contraction in order: four columns of a tile row per lane.
+template <int EDGE_M, int EDGE_N, typename E> __global__ __launch_bounds__(256) void product_join_kernel(ProductArgs p) {
+  constexpr int rows = 1024 / EDGE_N, slabs = EDGE_M / rows;
+  const int tile = blockIdx.x / slabs, r = (blockIdx.x - tile * slabs) * rows + threadIdx.x / (EDGE_N / 4);
+  const int c = (threadIdx.x % (EDGE_N / 4)) * 4;
+  int tm, tn;
+  tile_place(p, tile, tm, tn);
+  if (tm * EDGE_M + r >= p.M || tn * EDGE_N + c >= p.N) return;
+  const float* from = p.part + (long long)tile * p.pieces * (EDGE_M * EDGE_N) + r * EDGE_N + c;
   float v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
   for (int s = 0; s < p.pieces; ++s) {
-    const float4 x = *reinterpret_cast<const float4*>(from + (long long)s * (EDGE * EDGE));
+    const float4 x = *reinterpret_cast<const float4*>(from + (long long)s * (EDGE_M * EDGE_N));
     v[0] += x.x;
     v[1] += x.y;
     v[2] += x.z;
     v[3] += x.w;
   }
-  store_row<E, 4>(static_cast<E*>(p.out) + (long long)(tm * EDGE + r) * p.os + tn * EDGE + c, v, p.N - tn * EDGE - c, p.vec != 0,
+  store_row<E, 4>(static_cast<E*>(p.out) + (long long)(tm * EDGE_M + r) * p.os + tn * EDGE_N + c, v, p.N - tn * EDGE_N - c, p.vec != 0,
                   p.accumulate != 0);
 }
 
@@ -458,19 +516,22 @@ template <typename E, bool FAST> hipError_t launch_pack(const PackArgs& a, unsig
   hipLaunchKernelGGL((pack_blocks_kernel<E, FAST>), dim3(blocks), dim3(kPackThreads), 0, st, a);
   return hipGetLastError();
 }
-template <int NB, typename E> hipError_t launch_tiles(const ProductArgs& p, hipStream_t st) {
-  constexpr int lds = TileShape<NB>::lds, edge = TileShape<NB>::edge;
-  auto kern = product_tile_kernel<NB, std::is_same<E, float>::value, E>;
-  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+template <int MB, int NB, typename E> hipError_t launch_tiles(const ProductArgs& p, hipStream_t st) {
+  constexpr bool exact = std::is_same<E, float>::value;
+  using T = TileShape<MB, NB, exact>;
+  auto kern = product_tile_kernel<MB, NB, exact, E>;
+  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, T::lds);
   if (e != hipSuccess) return e;
   const unsigned total = unsigned(p.tiles_m) * unsigned(p.tiles_n);
-  hipLaunchKernelGGL(kern, dim3((total * p.pieces + kNumXcd - 1) / kNumXcd * kNumXcd), dim3(256), lds, st, p);
+  hipLaunchKernelGGL(kern, dim3((total * p.pieces + kNumXcd - 1) / kNumXcd * kNumXcd), dim3(256), T::lds, st, p);
   if (p.part)
-    hipLaunchKernelGGL((product_join_kernel<edge, E>), dim3(total * (edge * edge / 1024)), dim3(256), 0, st, p);
+    hipLaunchKernelGGL((product_join_kernel<T::edge_m, T::edge_n, E>), dim3(total * (T::edge_m * T::edge_n / 1024)), dim3(256), 0, st, p);
   return hipGetLastError();
 }
-template <typename E> hipError_t launch_product(const ProductArgs& p, int blocks, hipStream_t st) {
-  return blocks == 8 ? launch_tiles<8, E>(p, st) : launch_tiles<4, E>(p, st);
+template <typename E> hipError_t launch_product(const ProductArgs& p, bool large, hipStream_t st) {
+  if (!large) return launch_tiles<4, 4, E>(p, st);
+  if constexpr (std::is_same<E, float>::value) return launch_tiles<4, 8, E>(p, st);
+  else return launch_tiles<8, 8, E>(p, st);
 }
 
 RowSpan values_of(const adloco_blocks8* b) {
@@ -585,22 +646,23 @@ extern "C" int adloco_block_product(adloco_ctx* ctx, const adloco_blocks8* a, co
   DeviceScope scope(ctx);
   if (!scope.ok()) return fail(ctx, ADLOCO_EHIP, "block_product: device %d cannot be made current", ctx->device);
   hipStream_t st = static_cast<hipStream_t>(stream);
-  const int blocks = ctx->product_blocks ? ctx->product_blocks : 8;
-  const int64_t edge = 32 * blocks, tm = (a->rows + edge - 1) / edge, tn = (b->rows + edge - 1) / edge;
+  const bool large = ctx->product_blocks != 4;
+  const int64_t edge_m = large && dtype != ADLOCO_F32 ? 256 : 128, edge_n = large ? 256 : 128;
+  const int64_t tm = (a->rows + edge_m - 1) / edge_m, tn = (b->rows + edge_n - 1) / edge_n;
   if (tm * tn > 0xffffffLL) return fail(ctx, ADLOCO_EUNSUPPORTED, "block_product: too many tiles for one launch");
   p.tiles_m = int(tm);
   p.tiles_n = int(tn);
   p.pieces = ctx->product_pieces ? ctx->product_pieces : 1;
   if (p.pieces > p.steps) p.pieces = p.steps;
   if (p.pieces > 1) {
-    p.part = size_t(tm * tn * p.pieces) * size_t(edge * edge) * sizeof(float) <= kLayerScratch ? layer_scratch(ctx, st) : nullptr;
+    p.part = size_t(tm * tn * p.pieces) * size_t(edge_m * edge_n) * sizeof(float) <= kLayerScratch ? layer_scratch(ctx, st) : nullptr;
     if (!p.part) p.pieces = 1;
   }
-  const int64_t row = (p.pieces > 1 ? 4 : blocks) * (int64_t)es;
+  const int64_t row = (p.pieces > 1 ? 4 : edge_n / 32) * (int64_t)es;
   p.vec = reinterpret_cast<uintptr_t>(out) % row == 0 && os * (int64_t)es % row == 0;
   hipEvent_t ev = prof_begin(ctx, st);
-  const hipError_t e = dtype == ADLOCO_BF16 ? launch_product<__bf16>(p, blocks, st)
-                       : dtype == ADLOCO_F16 ? launch_product<_Float16>(p, blocks, st) : launch_product<float>(p, blocks, st);
+  const hipError_t e = dtype == ADLOCO_BF16 ? launch_product<__bf16>(p, large, st)
+                       : dtype == ADLOCO_F16 ? launch_product<_Float16>(p, large, st) : launch_product<float>(p, large, st);
   prof_end(ctx, kProfProduct, ev, st);
   if (e != hipSuccess) return fail(ctx, ADLOCO_EHIP, "block_product launch failed: %s", hipGetErrorString(e));
   return ADLOCO_OK;
