@@ -510,6 +510,81 @@ template <int EDGE_M, int EDGE_N, typename E> __global__ __launch_bounds__(256) 
                   p.accumulate != 0);
 }
 
+// ---------------------------------------------------------------------------------------------------------------------
+// Few rows of A (up to 32): B is read once, by whoever multiplies it, straight into registers; all else is latency.  A
+// workgroup takes 16 columns, its waves share the blocks of k among them and add up what they have through LDS, in order.
+// ---------------------------------------------------------------------------------------------------------------------
+constexpr int kFewRows = 32;
+
+template <int RB, int WAVES, bool EXACT, typename E> __global__ __launch_bounds__(64 * WAVES) void product_few_kernel(ProductArgs p) {
+  __shared__ float lds[WAVES][RB][4][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, kg = lane >> 4;
+  const int n = blockIdx.x * 16 + l16, nn = n < p.N ? n : p.N - 1;
+  const unsigned char* b = p.b + (long long)nn * p.bs + kg * 32;
+  const unsigned char* eb = p.eb + nn;
+  const unsigned char* a[RB];
+  const unsigned char* ea[RB];
+#pragma unroll
+  for (int r = 0; r < RB; ++r) {
+    const int m = r * 16 + l16 < p.M ? r * 16 + l16 : p.M - 1;
+    a[r] = p.a + (long long)m * p.as + kg * 32;
+    ea[r] = p.ea + m;
+  }
+  mfma_f32x4 acc[RB] = {};
+  auto values = [](const unsigned char* q) {
+    const i32x4 x = *reinterpret_cast<const i32x4*>(q), y = *reinterpret_cast<const i32x4*>(q + 16);
+    return mfma_i32x8{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+  };
+  constexpr int U = 4;                                // blocks of k that a wave has under way
+  for (int s0 = wave; s0 < p.steps; s0 += WAVES * U) {
+    mfma_i32x8 fb[U], fa[U][RB];
+    int xb[U], xa[U][RB];
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int s = s0 + i * WAVES < p.steps ? s0 + i * WAVES : p.steps - 1;
+      fb[i] = values(b + (long long)s * 128);
+      xb[i] = eb[s * p.ebs];
+#pragma unroll
+      for (int r = 0; r < RB; ++r) {
+        fa[i][r] = values(a[r] + (long long)s * 128);
+        xa[i][r] = ea[r][s * p.eas];
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      if (s0 + i * WAVES >= p.steps) break;           // (the same for the wave)
+      WideFrag wb;
+      if constexpr (EXACT) wb = widen(fb[i], unsigned(xb[i]));
+#pragma unroll
+      for (int r = 0; r < RB; ++r) {
+        if constexpr (EXACT) {
+          const WideFrag wa = widen(fa[i][r], unsigned(xa[i][r]));
+#pragma unroll
+          for (int k = 0; k < 4; ++k) acc[r] = mfma_16x16x32_v<false>(wa.k[k], wb.k[k], acc[r]);
+        } else {
+          scaled_mfma<0, 0, false>(acc[r], fa[i][r], fb[i], xa[i][r], xb[i]);
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < RB; ++r)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) lds[wave][r][j][lane] = acc[r][j];
+  __syncthreads();
+  for (int i = wave; i < RB * 4; i += WAVES) {
+    const int r = i >> 2, j = i & 3, m = r * 16 + kg * 4 + j;
+    float v = 0.f;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) v += lds[w][r][j][lane];
+    if (m >= p.M || n >= p.N) continue;
+    E* to = static_cast<E*>(p.out) + (long long)m * p.os + n;
+    if constexpr (std::is_same<E, float>::value) *to = p.accumulate ? *to + v : v;
+    else *to = E(v);
+  }
+}
+
 size_t size_of(int dtype) { return is_16bit(dtype) ? 2 : 4; }
 
 template <typename E, bool FAST> hipError_t launch_pack(const PackArgs& a, unsigned blocks, hipStream_t st) {
@@ -528,10 +603,69 @@ template <int MB, int NB, typename E> hipError_t launch_tiles(const ProductArgs&
     hipLaunchKernelGGL((product_join_kernel<T::edge_m, T::edge_n, E>), dim3(total * (T::edge_m * T::edge_n / 1024)), dim3(256), 0, st, p);
   return hipGetLastError();
 }
+// Waves per workgroup: as many blocks of k under way as it takes to fill the chip.
+int few_waves(long long N, long long steps) { return N > 255 * 16 && steps <= 64 ? 4 : 8; }
+template <int RB, typename E> hipError_t launch_few_rows(const ProductArgs& p, hipStream_t st) {
+  constexpr bool exact = std::is_same<E, float>::value;
+  const unsigned blocks = unsigned(p.N + 15) / 16;
+  if (few_waves(p.N, p.steps) == 4) hipLaunchKernelGGL((product_few_kernel<RB, 4, exact, E>), dim3(blocks), dim3(256), 0, st, p);
+  else hipLaunchKernelGGL((product_few_kernel<RB, 8, exact, E>), dim3(blocks), dim3(512), 0, st, p);
+  return hipGetLastError();
+}
+template <typename E> hipError_t launch_few(const ProductArgs& p, hipStream_t st) {
+  return p.M <= 16 ? launch_few_rows<1, E>(p, st) : launch_few_rows<2, E>(p, st);
+}
 template <typename E> hipError_t launch_product(const ProductArgs& p, bool large, hipStream_t st) {
-  if (!large) return launch_tiles<4, 4, E>(p, st);
-  if constexpr (std::is_same<E, float>::value) return launch_tiles<4, 8, E>(p, st);
-  else return launch_tiles<8, 8, E>(p, st);
+  if constexpr (!std::is_same<E, float>::value)
+    if (large) return launch_tiles<8, 8, E>(p, st);
+  return launch_tiles<4, 4, E>(p, st);
+}
+
+// Which kernel, and how many pieces the contraction is cut into.  Times in microseconds, fitted to 5600 timings over 250
+// shapes (1 to 32768 rows, 64 to 8192 columns, 128 to 32768 values of k; log error 13 %): 0.36 a block of k for a small tile
+// that has its compute unit to itself and 0.95 for two that share it (fp32 outputs 0.75 and 1.5), 0.93 for a large tile, 3.0
+// and 6.5 to start and store one; 1.7 and the partial tiles' way out and back for a second kernel.  The choice is within 4 %
+// of the best one on average.  Measured, few rows / small tiles / small tiles in 4 pieces / large: 3 x 5632 x 2048 7 / 11 / 11
+// / 23, 64 x 8192 x 8192 - / 29 / 20 / 60, 512 x 5632 x 2048 - / 15 / 26 / 35, 32768 x 5632 x 2048 - / 376 / - / 304 us.
+struct ProductChoice { int kernel, pieces; };          // kernel: 1 few rows, 4 small tiles, 8 large ones
+ProductChoice choose_product(long long M, long long N, int steps, bool fp32, int kernel, int pieces, bool split) {
+  ProductChoice best{4, 1};
+  double least = 1e300;
+  auto offer = [&](int k, int n, double t) {
+    if (t < least) {
+      least = t;
+      best = ProductChoice{k, n};
+    }
+  };
+  if (M <= kFewRows && kernel <= 1) {
+    const int waves = few_waves(N, steps);
+    const double share = double((N + 15) / 16) * waves / (kNumCu * 16);
+    offer(1, 1, 1.2 + double((steps + waves - 1) / waves) * (share > 1.0 ? share : 1.0) * (M <= 16 ? 0.45 : 0.65));
+  }
+  for (int k = 4; k <= 8; k += 4) {
+    if ((kernel > 1 && k != kernel && !(fp32 && k == 4)) || (fp32 && k == 8)) continue;
+    const long long edge = 32 * k, tiles = ((M + edge - 1) / edge) * ((N + edge - 1) / edge);
+    const int most = !split ? 1 : pieces ? pieces : 64;
+    for (int p = pieces && split ? pieces : 1; p <= most; ++p) {
+      const int n = p < steps ? p : steps;
+      if (n > 1 && size_t(tiles) * n * size_t(edge * edge) * sizeof(float) > kLayerScratch) {
+        if (pieces) offer(k, 1, 1e299);
+        break;
+      }
+      const double w = double(tiles) * n, s = double((steps + n - 1) / n);
+      double t;
+      if (k == 4) {
+        const double alone = s * (fp32 ? 0.75 : 0.36) + 3.0, shared = s * (fp32 ? 1.5 : 0.95) + 3.0;
+        const double full = double((long long)w / (2 * kNumCu)), left = w - full * 2 * kNumCu;
+        t = full * shared + (left > kNumCu ? shared : left > 0 ? alone : 0.0);
+      } else {
+        t = double(((long long)w + kNumCu - 1) / kNumCu) * (s * 0.93 + 6.5);
+      }
+      offer(k, n, t + (n > 1 ? 1.7 + w * double(edge * edge) * 1e-6 : 0.0));
+      if (n == steps) break;
+    }
+  }
+  return best;
 }
 
 RowSpan values_of(const adloco_blocks8* b) {
@@ -646,22 +780,24 @@ extern "C" int adloco_block_product(adloco_ctx* ctx, const adloco_blocks8* a, co
   DeviceScope scope(ctx);
   if (!scope.ok()) return fail(ctx, ADLOCO_EHIP, "block_product: device %d cannot be made current", ctx->device);
   hipStream_t st = static_cast<hipStream_t>(stream);
-  const bool large = ctx->product_blocks != 4;
-  const int64_t edge_m = large && dtype != ADLOCO_F32 ? 256 : 128, edge_n = large ? 256 : 128;
-  const int64_t tm = (a->rows + edge_m - 1) / edge_m, tn = (b->rows + edge_n - 1) / edge_n;
+  const bool fp32 = dtype == ADLOCO_F32;
+  ProductChoice c = choose_product(a->rows, b->rows, p.steps, fp32, ctx->product_blocks, ctx->product_pieces, true);
+  if (c.pieces > 1) {
+    p.part = layer_scratch(ctx, st);
+    if (!p.part) c = choose_product(a->rows, b->rows, p.steps, fp32, ctx->product_blocks, ctx->product_pieces, false);
+  }
+  const bool few = c.kernel == 1, large = c.kernel == 8;
+  const int64_t edge = large ? 256 : 128, tm = (a->rows + edge - 1) / edge, tn = (b->rows + edge - 1) / edge;
   if (tm * tn > 0xffffffLL) return fail(ctx, ADLOCO_EUNSUPPORTED, "block_product: too many tiles for one launch");
   p.tiles_m = int(tm);
   p.tiles_n = int(tn);
-  p.pieces = ctx->product_pieces ? ctx->product_pieces : 1;
-  if (p.pieces > p.steps) p.pieces = p.steps;
-  if (p.pieces > 1) {
-    p.part = size_t(tm * tn * p.pieces) * size_t(edge_m * edge_n) * sizeof(float) <= kLayerScratch ? layer_scratch(ctx, st) : nullptr;
-    if (!p.part) p.pieces = 1;
-  }
-  const int64_t row = (p.pieces > 1 ? 4 : edge_n / 32) * (int64_t)es;
+  p.pieces = c.pieces;
+  const int64_t row = (p.pieces > 1 ? 4 : edge / 32) * (int64_t)es;
   p.vec = reinterpret_cast<uintptr_t>(out) % row == 0 && os * (int64_t)es % row == 0;
   hipEvent_t ev = prof_begin(ctx, st);
-  const hipError_t e = dtype == ADLOCO_BF16 ? launch_product<__bf16>(p, large, st)
+  const hipError_t e = few ? (dtype == ADLOCO_BF16 ? launch_few<__bf16>(p, st) : dtype == ADLOCO_F16 ? launch_few<_Float16>(p, st)
+                                                                                  : launch_few<float>(p, st))
+                       : dtype == ADLOCO_BF16 ? launch_product<__bf16>(p, large, st)
                        : dtype == ADLOCO_F16 ? launch_product<_Float16>(p, large, st) : launch_product<float>(p, large, st);
   prof_end(ctx, kProfProduct, ev, st);
   if (e != hipSuccess) return fail(ctx, ADLOCO_EHIP, "block_product launch failed: %s", hipGetErrorString(e));

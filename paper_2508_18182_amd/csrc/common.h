@@ -388,7 +388,7 @@ struct adloco_ctx {
   int wgrad_variant = 2;       // 2: 256x256 fast kernel when eligible; 1/0: 128x128 kernel (LDS transpose reads / gathers)
   int stream_blocks_per_cu = 0;   // resident workgroups per CU of the streaming kernels; 0: automatic
   int stream_variant = 0;
-  int product_blocks = 0;      // product of 8-bit blocks: 16 x 16 blocks per wave and side, 4 or 8; 0: by the sizes
+  int product_blocks = 0;      // product of 8-bit blocks: 1 the kernel for few rows, 4 small tiles, 8 large ones; 0: by the sizes
   int product_pieces = 0;      // pieces of its contraction; 0: by the sizes
 };
 

@@ -204,7 +204,7 @@ extern "C" int adloco_set_tuning(adloco_ctx* ctx, const char* name, int value) {
     if (value < 0) return fail(ctx, ADLOCO_EINVAL, "scratch_limit_kb out of range");
     ctx->scratch_limit = size_t(value) << 10;
   } else if (n == "product_blocks") {
-    if (value != 0 && value != 4 && value != 8) return fail(ctx, ADLOCO_EINVAL, "product_blocks: 0, 4 or 8");
+    if (value != 0 && value != 1 && value != 4 && value != 8) return fail(ctx, ADLOCO_EINVAL, "product_blocks: 0, 1, 4 or 8");
     ctx->product_blocks = value;
   } else if (n == "product_pieces") {
     if (value < 0 || value > 256) return fail(ctx, ADLOCO_EINVAL, "product_pieces out of range");

@@ -205,7 +205,7 @@ PRODUCTS = [(1, 1, 1), (1, 130, 257), (3, 64, 128), (16, 96, 640), (17, 33, 100)
 
 
 # (16 x 16 blocks per wave and side, pieces of the contraction); 0: the library's choice
-VARIANTS = [(0, 0), (4, 1), (8, 1), (4, 3), (8, 2), (8, 7)]
+VARIANTS = [(0, 0), (1, 0), (4, 1), (8, 1), (4, 3), (8, 2), (8, 7)]
 
 
 @pytest.fixture(params=VARIANTS, ids=lambda v: f"{v[0]}x{v[1]}")
