@@ -601,41 +601,53 @@ class Blocks8:
 
 
 def _on(ctx: Context, t, name: str):
-    if not t.is_cuda or t.device.index != ctx.device:
+    if t.get_device() != ctx.device:              # (-1 for a tensor in host memory)
         raise ValueError(f"{name} must live on the context's GPU, cuda:{ctx.device}")
 
 
-def _layer_stream(ctx: Context, stream):
+def _layer_stream(ctx: Context, stream) -> int:
     import torch
-    return C.c_void_p((torch.cuda.current_stream(ctx.device) if stream is None else stream).cuda_stream)
+    return torch._C._cuda_getCurrentRawStream(ctx.device) if stream is None else stream.cuda_stream
 
 
 def _blocks8(ctx: Context, b: Optional[Blocks8], name: str):
     """Descriptor of a Blocks8, or None."""
-    import torch
     if b is None:
         return None
-    for t, nm, rows, width in ((b.data, "data", b.rows, -(-b.cols // 128) * 128), (b.exponent, "exponent", -(-b.cols // 128), b.rows)):
-        _on(ctx, t, f"{name}.{nm}")
-        if t.dtype != torch.uint8 or t.dim() != 2 or t.shape[0] < rows or t.shape[1] < width or (t.shape[1] > 1 and t.stride(1) != 1):
-            raise ValueError(f"{name}.{nm} must be uint8 [>= {rows}, >= {width}] with unit stride along its rows, got "
-                             f"{tuple(t.shape)} {t.dtype}")
-    return Blocks8Desc(b.data.data_ptr(), b.exponent.data_ptr(), b.rows, b.cols,
-                       b.data.stride(0) if b.data.shape[0] > 1 else b.data.shape[1],
-                       b.exponent.stride(0) if b.exponent.shape[0] > 1 else b.exponent.shape[1])
+    data, exponent, rows, cols = b.data, b.exponent, b.rows, b.cols
+    wide = (cols + 127) // 128 * 128
+    _on(ctx, data, name)
+    _on(ctx, exponent, name)
+    if not (_is_bytes(data, rows, wide) and _is_bytes(exponent, wide // 128, rows)):
+        raise ValueError(f"{name}: data must be uint8 [>= {rows}, >= {wide}] and exponent uint8 [>= {wide // 128}, >= {rows}], "
+                         f"both with unit stride along their rows; got {tuple(data.shape)} {data.dtype} and "
+                         f"{tuple(exponent.shape)} {exponent.dtype}")
+    return Blocks8Desc(data.data_ptr(), exponent.data_ptr(), rows, cols, _row_bytes(data), _row_bytes(exponent))
 
 
-def _matrix(ctx: Context, t, name: str, like=None):
-    """(address, row stride) of a tensor [..., d] whose rows are a uniform stride apart; (None, 0) for None.  like: a
-    tensor whose shape and type it must have."""
+def _is_bytes(t, rows: int, width: int) -> bool:
+    import torch
+    if t.dtype is not torch.uint8 or t.dim() != 2:
+        return False
+    r, w = t.shape
+    return r >= rows and w >= width and (w <= 1 or t.stride(1) == 1)
+
+
+def _row_bytes(t) -> int:
+    return t.stride(0) if t.size(0) > 1 else t.size(1)
+
+
+def _matrix(ctx: Context, t, name: str, shape=None, dtype=None):
+    """(address, row stride; 0: rows without gaps) of a tensor [..., d] whose rows are a uniform stride apart; (None, 0) for
+    None.  shape, dtype: what it has to be."""
     if t is None:
         return None, 0
     _on(ctx, t, name)
-    if t.dim() < 1 or (like is not None and (t.shape != like.shape or t.dtype != like.dtype)):
-        raise ValueError(f"{name} must be {'a matrix' if like is None else f'{tuple(like.shape)} {like.dtype}'}, got "
+    if t.dim() < 1 or (shape is not None and (t.shape != shape or t.dtype is not dtype)):
+        raise ValueError(f"{name} must be {'a matrix' if shape is None else f'{tuple(shape)} {dtype}'}, got "
                          f"{tuple(t.shape)} {t.dtype}")
     if t.is_contiguous():
-        return t.data_ptr(), t.shape[-1]
+        return t.data_ptr(), 0
     if t.shape[-1] > 1 and t.stride(-1) != 1:
         raise ValueError(f"{name} needs unit stride in its last dimension")
     stride = rows = None
@@ -648,28 +660,32 @@ def _matrix(ctx: Context, t, name: str, like=None):
             raise ValueError(f"{name}: its rows must be evenly spaced")
         else:
             rows *= t.shape[i]
-    return t.data_ptr(), t.shape[-1] if stride is None else stride
+    if stride is None:
+        return t.data_ptr(), 0
+    if stride < 1:                                # an expanded tensor: every row the same one
+        raise ValueError(f"{name}: its rows must not share memory")
+    return t.data_ptr(), stride
 
 
 _LAYER_DTYPES = {}
 
 
-def _layer_dtype(t, name: str) -> int:
+def _layer_dtype(dtype, name: str) -> int:
     import torch
     if not _LAYER_DTYPES:
         _LAYER_DTYPES.update({torch.float32: ADLOCO_F32, torch.bfloat16: ADLOCO_BF16, torch.float16: ADLOCO_F16})
-    code = _LAYER_DTYPES.get(t.dtype)
+    code = _LAYER_DTYPES.get(dtype)
     if code is None:
-        raise TypeError(f"{name} has dtype {t.dtype}, expected float32, bfloat16 or float16")
+        raise TypeError(f"{name} has dtype {dtype}, expected float32, bfloat16 or float16")
     return code
 
 
-def _rows(t) -> int:
-    return t.numel() // t.shape[-1] if t.shape[-1] else 0
+def _rows_of(t, shape, d: int) -> int:
+    return shape[0] if len(shape) == 2 else t.numel() // d if d else 0
 
 
 def _mask(p: float, seed: int, first_row: int):
-    return DropoutMask(float(p), int(seed) & 0xFFFFFFFFFFFFFFFF, int(first_row)) if p else None
+    return DropoutMask(p, seed & 0xFFFFFFFFFFFFFFFF, first_row) if p else None
 
 
 def _gain(ctx: Context, gain, d: int):
@@ -677,7 +693,7 @@ def _gain(ctx: Context, gain, d: int):
     if gain is None:
         return None
     _on(ctx, gain, "gain")
-    if gain.dtype != torch.float32 or gain.numel() != d or not gain.is_contiguous():
+    if gain.dtype is not torch.float32 or gain.numel() != d or not gain.is_contiguous():
         raise ValueError(f"gain must be a contiguous fp32 tensor of {d} values")
     return gain.data_ptr()
 
@@ -686,30 +702,34 @@ def adloco_dropout(ctx: Context, x, out, p: float, seed: int, first_row: int = 0
     """out = residual + dropout(x) (or dropout(x)); tensors [..., d] of one shape and type.  out may be x or residual.
     The mask of a row depends on seed, its number first_row + i and the column alone: the same call on a gradient is the
     backward pass."""
-    code = _layer_dtype(x, "x")
+    shape, dtype = x.shape, x.dtype
+    code = _layer_dtype(dtype, "x")
     px, sx = _matrix(ctx, x, "x")
-    pr, sr = _matrix(ctx, residual, "residual", x)
-    po, so = _matrix(ctx, out, "out", x)
-    mask = DropoutMask(float(p), int(seed) & 0xFFFFFFFFFFFFFFFF, int(first_row))
-    ctx._check(load_library().adloco_dropout(ctx._h, px, sx, pr, sr, po, so, _rows(x), x.shape[-1], code, C.byref(mask),
+    pr, sr = _matrix(ctx, residual, "residual", shape, dtype)
+    po, so = _matrix(ctx, out, "out", shape, dtype)
+    d = shape[-1]
+    mask = DropoutMask(p, seed & 0xFFFFFFFFFFFFFFFF, first_row)
+    ctx._check(load_library().adloco_dropout(ctx._h, px, sx, pr, sr, po, so, _rows_of(x, shape, d), d, code, mask,
                                              _layer_stream(ctx, stream)))
 
 
 def adloco_pack_blocks(ctx: Context, x, along: Optional[Blocks8] = None, across: Optional[Blocks8] = None, stream=None):
     """x [..., cols] to 8-bit blocks along its rows (along: rows x cols) and / or across them (across: cols x rows)."""
-    code = _layer_dtype(x, "x")
+    shape = x.shape
+    code = _layer_dtype(x.dtype, "x")
     px, sx = _matrix(ctx, x, "x")
     al, ac = _blocks8(ctx, along, "along"), _blocks8(ctx, across, "across")
-    ctx._check(load_library().adloco_pack_blocks(ctx._h, px, sx, _rows(x), x.shape[-1], code, al, ac,
+    ctx._check(load_library().adloco_pack_blocks(ctx._h, px, sx, _rows_of(x, shape, shape[-1]), shape[-1], code, al, ac,
                                                  _layer_stream(ctx, stream)))
 
 
 def adloco_block_product(ctx: Context, a: Blocks8, b: Blocks8, out, flags: int = 0, stream=None):
     """out [a.rows, b.rows] (fp32, bf16 or fp16) = a b^T; with ADLOCO_ACCUMULATE (fp32) added to out."""
-    code = _layer_dtype(out, "out")
+    shape = out.shape
+    code = _layer_dtype(out.dtype, "out")
     da, db = _blocks8(ctx, a, "a"), _blocks8(ctx, b, "b")
-    if out.shape[-1] != b.rows or out.numel() != a.rows * b.rows:
-        raise ValueError(f"out must be [{a.rows}, {b.rows}], got {tuple(out.shape)}")
+    if not shape or shape[-1] != b.rows or out.numel() != a.rows * b.rows:
+        raise ValueError(f"out must be [{a.rows}, {b.rows}], got {tuple(shape)}")
     po, so = _matrix(ctx, out, "out")
     ctx._check(load_library().adloco_block_product(ctx._h, da, db, po, so, code, flags, _layer_stream(ctx, stream)))
 
@@ -718,15 +738,15 @@ def adloco_rms_norm(ctx: Context, x, gain, eps: float, y=None, y8: Optional[Bloc
                     p: float = 0.0, seed: int = 0, first_row: int = 0, stream=None):
     """h_out = h = residual + dropout(x); y (and y8, in 8-bit blocks) = h / sqrt(mean(h^2) + eps) * gain.  Tensors
     [..., d] of one shape and type, gain fp32 [d] or None; outputs that are None are not written."""
-    code = _layer_dtype(x, "x")
-    d = x.shape[-1]
-    io = NormIo()
-    io.gain = _gain(ctx, gain, d)
-    io.x, io.x_row_stride = _matrix(ctx, x, "x")
-    io.residual, io.residual_row_stride = _matrix(ctx, residual, "residual", x)
-    io.h, io.h_row_stride = _matrix(ctx, h_out, "h_out", x)
-    io.y, io.y_row_stride = _matrix(ctx, y, "y", x)
-    ctx._check(load_library().adloco_rms_norm(ctx._h, C.byref(io), _rows(x), d, code, eps, _mask(p, seed, first_row),
+    shape, dtype = x.shape, x.dtype
+    code = _layer_dtype(dtype, "x")
+    px, sx = _matrix(ctx, x, "x")
+    pr, sr = _matrix(ctx, residual, "residual", shape, dtype)
+    ph, sh = _matrix(ctx, h_out, "h_out", shape, dtype)
+    py, sy = _matrix(ctx, y, "y", shape, dtype)
+    d = shape[-1]
+    io = NormIo(px, pr, _gain(ctx, gain, d), ph, py, sx, sr, sh, sy)
+    ctx._check(load_library().adloco_rms_norm(ctx._h, io, _rows_of(x, shape, d), d, code, eps, _mask(p, seed, first_row),
                                               _blocks8(ctx, y8, "y8"), _layer_stream(ctx, stream)))
 
 
@@ -735,23 +755,23 @@ def adloco_rms_norm_backward(ctx: Context, h, gain, dy, eps: float, dh_out=None,
     """Gradient of the norm: dh_out = dh_in + d y / d h^T dy, dx_out = dropout(dh_out), gain_sums fp32 [B, d] = the gain's
     gradient of every sample, whose rows are h's in order (B divides their number; None: one sample)."""
     import torch
-    code = _layer_dtype(h, "h")
-    d, rows = h.shape[-1], _rows(h)
-    B = 1
-    io = NormBackwardIo()
+    shape, dtype = h.shape, h.dtype
+    code = _layer_dtype(dtype, "h")
+    ph, sh = _matrix(ctx, h, "h")
+    py, sy = _matrix(ctx, dy, "dy", shape, dtype)
+    pi, si = _matrix(ctx, dh_in, "dh_in", shape, dtype)
+    po, so = _matrix(ctx, dh_out, "dh_out", shape, dtype)
+    px, sx = _matrix(ctx, dx_out, "dx_out", shape, dtype)
+    d = shape[-1]
+    rows, B, sums = _rows_of(h, shape, d), 1, None
     if gain_sums is not None:
         _on(ctx, gain_sums, "gain_sums")
-        B = gain_sums.shape[0]
-        if gain_sums.dtype != torch.float32 or tuple(gain_sums.shape) != (B, d) or not gain_sums.is_contiguous() or (B and rows % B):
+        B = gain_sums.shape[0] if gain_sums.dim() == 2 else -1
+        if gain_sums.dtype is not torch.float32 or B < 0 or gain_sums.shape[1] != d or not gain_sums.is_contiguous() or (B == 0 and rows) or (B and rows % B):
             raise ValueError(f"gain_sums must be a contiguous fp32 tensor [B, {d}] with B dividing {rows} rows")
-        io.gain_sums = gain_sums.data_ptr()
-    io.gain = _gain(ctx, gain, d)
-    io.h, io.h_row_stride = _matrix(ctx, h, "h")
-    io.dy, io.dy_row_stride = _matrix(ctx, dy, "dy", h)
-    io.dh_in, io.dh_in_row_stride = _matrix(ctx, dh_in, "dh_in", h)
-    io.dh, io.dh_row_stride = _matrix(ctx, dh_out, "dh_out", h)
-    io.dx, io.dx_row_stride = _matrix(ctx, dx_out, "dx_out", h)
-    ctx._check(load_library().adloco_rms_norm_backward(ctx._h, C.byref(io), B, rows // B if B else 0, d, code, eps,
+        sums = gain_sums.data_ptr()
+    io = NormBackwardIo(ph, py, pi, _gain(ctx, gain, d), po, px, sums, sh, sy, si, so, sx)
+    ctx._check(load_library().adloco_rms_norm_backward(ctx._h, io, B, rows // B if B else 0, d, code, eps,
                                                        _mask(p, seed, first_row), _layer_stream(ctx, stream)))
 
 

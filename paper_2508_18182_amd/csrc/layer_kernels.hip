@@ -56,14 +56,14 @@ struct NormArgs {
   long long qs, es;
   long long rows;
   int d, wide;               // wide: d up to whole blocks where they are written, else d
-  float inv_d, eps;
+  double inv_d, eps;
   DropoutArgs m;
 };
 
 constexpr float kTiny = 1.262177448353619e-29f;   // 2^-96: 16384 squares of the largest fp32 number fit
 
 // Sums over the row of a few values at once; `slot` alternates from row to row, so that one barrier is enough.
-template <int WAVES, int N> __device__ __forceinline__ void row_sums(float (&s)[N], float (*lds)[8][2], int slot) {
+template <int WAVES, int N, typename F> __device__ __forceinline__ void row_sums(F (&s)[N], F (*lds)[8][N], int slot) {
 #pragma unroll
   for (int k = 0; k < N; ++k) s[k] = sum64(s[k]);
   if constexpr (WAVES > 1) {
@@ -92,7 +92,7 @@ __device__ __forceinline__ void load_gain(const float* gain, int c, int d, bool 
 }
 
 template <typename E, int NV, int WAVES, bool FAST> __global__ __launch_bounds__(64 * WAVES) void rms_norm_kernel(NormArgs a) {
-  __shared__ float lds[4][8][2];
+  __shared__ double lds[4][8][1];
   int slot = 0;
   const int c0 = threadIdx.x * 8;
   float g[NV][8];
@@ -118,39 +118,52 @@ template <typename E, int NV, int WAVES, bool FAST> __global__ __launch_bounds__
     if (a.h)
 #pragma unroll
       for (int i = 0; i < NV; ++i) store_eight<E, FAST>(static_cast<E*>(a.h) + row * a.hs, c0 + i * 512 * WAVES, a.d, h[i]);
-    float s[1] = {0.f}, eps = a.eps;
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) s[0] = fmaf(h[i][j], h[i][j], s[0]);
-    row_sums<WAVES, 1>(s, lds, slot++ & 3);
-    if (!(s[0] <= 3.402823466e38f)) {               // (the same for the whole row)
-      s[0] = 0.f;
-      eps *= kTiny * kTiny;
+    // One factor for the whole row, and 8-bit outputs that change by a whole step where a value lies next to the middle of two:
+    // the sum over the lanes and the root are formed in fp64 (once per row), and the products with the root's and their own
+    // rounding errors carried along, up to the one rounding of the output.
+    auto squares = [&] {
+      float q = 0.f;
 #pragma unroll
       for (int i = 0; i < NV; ++i)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          h[i][j] *= kTiny;
-          s[0] = fmaf(h[i][j], h[i][j], s[0]);
-        }
+        for (int j = 0; j < 8; ++j) q = fmaf(h[i][j], h[i][j], q);
+      return q;
+    };
+    double s[1] = {squares()}, eps = a.eps;
+    row_sums<WAVES, 1>(s, lds, slot++ & 3);
+    if (!(s[0] <= 3.402823466e38)) {                // (the same for the whole row)
+      eps *= double(kTiny) * kTiny;
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) h[i][j] *= kTiny;
+      s[0] = squares();
       row_sums<WAVES, 1>(s, lds, slot++ & 3);
     }
-    const float rs = rsqrtf(fmaf(s[0], a.inv_d, eps));
+    const double root = rsqrt(s[0] * a.inv_d + eps);
+    const float r_hi = float(root), r_lo = float(root - double(r_hi));
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
+      float odd[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) h[i][j] = h[i][j] * rs * g[i][j];
+      for (int j = 0; j < 8; ++j) {
+        const float n = h[i][j] * r_hi, rest = fmaf(h[i][j], r_lo, fmaf(h[i][j], r_hi, -n)) * g[i][j];
+        h[i][j] = fmaf(n, g[i][j], rest);
+        odd[j] = round_to_odd(h[i][j], fmaf(n, g[i][j], -h[i][j]) + rest);
+      }
       const int c = c0 + i * 512 * WAVES;
-      if (a.y) store_eight<E, FAST>(static_cast<E*>(a.y) + row * a.ys, c, a.d, h[i]);
+      if (a.y) {
+        if constexpr (std::is_same<E, float>::value) store_eight<E, FAST>(static_cast<E*>(a.y) + row * a.ys, c, a.d, h[i]);
+        else store_eight<E, FAST>(static_cast<E*>(a.y) + row * a.ys, c, a.d, odd);
+      }
       if (a.q) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) h[i][j] = c + j < a.d ? h[i][j] : 0.f;       // (in a row whose norm is not finite, 0 * NaN)
+        for (int j = 0; j < 8; ++j) odd[j] = c + j < a.d ? odd[j] : 0.f;       // (in a row whose norm is not finite, 0 * NaN)
         bool any;
-        const unsigned e = row_block(h[i], any);
+        const unsigned e = row_block(odd, any);
         if (c < a.wide) {
-          uint2 o = pack_eight(h[i], e);
-          if (any) mark_eight(h[i], o);
+          uint2 o = pack_eight(odd, e);
+          if (any) mark_eight(odd, o);
           *reinterpret_cast<uint2*>(a.q + row * a.qs + c) = o;
           if ((threadIdx.x & 15) == 0) a.e[(long long)(c >> 7) * a.es + row] = (unsigned char)e;
         }
@@ -489,8 +502,8 @@ extern "C" int adloco_rms_norm(adloco_ctx* ctx, const adloco_norm_io* io, int64_
     a.es = y8->exponent_stride;
     a.wide = int((d + 127LL) / 128 * 128);
   }
-  a.inv_d = float(1.0 / d);
-  a.eps = float(eps);
+  a.inv_d = 1.0 / d;
+  a.eps = eps;
   DeviceScope scope(ctx);
   if (!scope.ok()) return fail(ctx, ADLOCO_EHIP, "rms_norm: device %d cannot be made current", ctx->device);
   hipStream_t st = static_cast<hipStream_t>(stream);

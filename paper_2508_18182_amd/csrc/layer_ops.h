@@ -1,6 +1,8 @@
 // Device arithmetic shared by the layer operators: rows of eight values, the dropout mask, 8-bit blocks.
 #pragma once
 
+#include <type_traits>
+
 #include "common.h"
 
 namespace adloco {
@@ -132,6 +134,15 @@ __device__ __forceinline__ void mark_eight(const float (&v)[8], uint2& o) {
   mark_four(v[0], v[1], v[2], v[3], o.x);
   mark_four(v[4], v[5], v[6], v[7], o.y);
 }
+// y, the fp32 rounding of y + rest, with its last bit set where something was rounded away (towards what it was): rounded
+// once more to fewer bits, it gives what y + rest gives.  Without it, one value in 2^20 comes to lie just between two e4m3
+// values by its first rounding, and goes a whole step the wrong way half the time.
+__device__ __forceinline__ float round_to_odd(float y, float rest) {
+  const unsigned u = __float_as_uint(y);
+  const int towards = int((__float_as_uint(rest) ^ u)) >> 31 | 1;        // away from zero: 1, towards it: -1
+  const bool cut = (rest < 0.f || rest > 0.f) && (u & 1u) == 0u && (u & 0x7fffffffu) != 0u;
+  return __uint_as_float(cut ? u + unsigned(towards) : u);
+}
 // Maximum over groups of 16 lanes, in all of them.  All lanes of a group have to be there.
 __device__ __forceinline__ unsigned max16(unsigned v) {
 #define ADLOCO_ROR_MAX(n) v = larger(v, unsigned(__builtin_amdgcn_update_dpp(0, int(v), 0x120 + n, 0xf, 0xf, false)))
@@ -158,6 +169,23 @@ __device__ __forceinline__ float sum64(float v) {
   ADLOCO_ROR_ADD(2);
   ADLOCO_ROR_ADD(1);
 #undef ADLOCO_ROR_ADD
+  v += __shfl_xor(v, 16, 64);
+  v += __shfl_xor(v, 32, 64);
+  return v;
+}
+
+// The same in fp64.
+__device__ __forceinline__ double sum64(double v) {
+  auto ror = [](double x, auto n) {
+    const unsigned long long u = __double_as_longlong(x);
+    const unsigned lo = __builtin_amdgcn_update_dpp(0, int(unsigned(u)), 0x120 + decltype(n)::value, 0xf, 0xf, false);
+    const unsigned hi = __builtin_amdgcn_update_dpp(0, int(unsigned(u >> 32)), 0x120 + decltype(n)::value, 0xf, 0xf, false);
+    return __longlong_as_double((unsigned long long)hi << 32 | lo);
+  };
+  v += ror(v, std::integral_constant<int, 8>{});
+  v += ror(v, std::integral_constant<int, 4>{});
+  v += ror(v, std::integral_constant<int, 2>{});
+  v += ror(v, std::integral_constant<int, 1>{});
   v += __shfl_xor(v, 16, 64);
   v += __shfl_xor(v, 32, 64);
   return v;
