@@ -67,7 +67,7 @@ extern "C" {
 #define ADLOCO_KIND_LINEAR      0x00u /* weight W [d_out, d_in] of a linear layer (the default)  */
 #define ADLOCO_KIND_VECTOR      0x10u /* vector p [d_out] used element-wise: a bias or a gain    */
 #define ADLOCO_KIND_EMBED       0x20u /* embedding table E [d_in, d_out], a = int32 token ids    */
-#define ADLOCO_KIND_SAMPLE_SUMS 0x30u /* vector p [d_out] whose per-sample gradients are at hand   */
+#define ADLOCO_KIND_SAMPLE_SUMS 0x40u /* vector p [d_out] whose per-sample gradients are at hand   */
 #define ADLOCO_KIND_MASK        0xf0u
 #define ADLOCO_BROADCAST        0x1u  /* outer_step: also write the new outer model into theta_k */
 #define ADLOCO_BIASED_VAR       0x1u  /* norm_test: variance normalised by 1/B instead of 1/(B-1)*/

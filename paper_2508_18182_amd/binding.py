@@ -16,7 +16,7 @@ ADLOCO_F32, ADLOCO_BF16, ADLOCO_F16 = 0, 1, 2
 ADLOCO_ACCUMULATE = 0x1
 ADLOCO_SUM_ONLY = 0x2
 ADLOCO_GRAD_PROVIDED = 0x1
-ADLOCO_KIND_LINEAR, ADLOCO_KIND_VECTOR, ADLOCO_KIND_EMBED, ADLOCO_KIND_SAMPLE_SUMS = 0x00, 0x10, 0x20, 0x30
+ADLOCO_KIND_LINEAR, ADLOCO_KIND_VECTOR, ADLOCO_KIND_EMBED, ADLOCO_KIND_SAMPLE_SUMS = 0x00, 0x10, 0x20, 0x40
 ADLOCO_BROADCAST = 0x1
 ADLOCO_BIASED_VAR = 0x1
 ADLOCO_ALLOW_SHRINK = 0x2
