@@ -247,26 +247,19 @@ __device__ __forceinline__ void scaled_mfma(mfma_f32x4& c, const mfma_i32x8& a, 
   else
     c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, SEL_A, ea, SEL_B, eb);
 }
-template <typename E, int NB> __device__ __forceinline__ void store_row(E* p, const float (&v)[NB], int left, bool vec, bool accumulate) {
+template <typename E, int NB> __device__ __forceinline__ void store_row(E* p, const float (&v)[NB], bool accumulate) {
   typedef __attribute__((ext_vector_type(NB))) E row;
-  if (vec && left >= NB) {
-    row r, old;
-    if constexpr (std::is_same<E, float>::value)
-      if (accumulate) old = *reinterpret_cast<const row*>(p);
+  row r;
+  if constexpr (std::is_same<E, float>::value) {
+    row old = {};
+    if (accumulate) old = *reinterpret_cast<const row*>(p);
 #pragma unroll
-    for (int n = 0; n < NB; ++n) {
-      if constexpr (std::is_same<E, float>::value) r[n] = accumulate ? old[n] + v[n] : v[n];
-      else r[n] = E(v[n]);
-    }
-    *reinterpret_cast<row*>(p) = r;
-    return;
+    for (int n = 0; n < NB; ++n) r[n] = accumulate ? old[n] + v[n] : v[n];
+  } else {
+#pragma unroll
+    for (int n = 0; n < NB; ++n) r[n] = E(v[n]);
   }
-#pragma unroll
-  for (int n = 0; n < NB; ++n)
-    if (n < left) {
-      if constexpr (std::is_same<E, float>::value) p[n] = accumulate ? p[n] + v[n] : v[n];
-      else p[n] = E(v[n]);
-    }
+  *reinterpret_cast<row*>(p) = r;
 }
 
 template <int MB, int NB, bool EXACT> struct TileShape {
@@ -470,22 +463,65 @@ __global__ __launch_bounds__(256, (TileShape<MB, NB, EXACT>::resident)) void pro
   if (n_steps & 1) step(0, h0, h1);
 
   if constexpr (pinned) mfma_fence(acc);
-  // element j of block (m, n): row (kg * 4 + j) * MB + m of the wave tile, column l16 * NB + n
-  float* const part = p.part ? p.part + ((long long)tile * p.pieces + piece) * (T::edge_m * T::edge_n) + wn + l16 * NB : nullptr;
-  E* const out = static_cast<E*>(p.out) + (long long)m0 * p.os + n0 + wn + l16 * NB;
-  const int left = p.N - n0 - wn - l16 * NB;
+  // Element j of block (m, n): row (kg * 4 + j) * MB + m of the wave tile, column l16 * NB + n.  Three ways out, each short
+  // enough for the instruction cache (checks woven into one of them: 60 KB of code, 4 us a tile).
+  auto rows_out = [&](int first, int count, auto put) {
 #pragma unroll
-  for (int m = 0; m < MB; ++m)
+    for (int m = 0; m < MB; ++m)
+      if (m >= first && m < first + count)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int r = wm + (kg * 4 + j) * MB + m;
-      float v[NB];
+        for (int j = 0; j < 4; ++j) {
+          float v[NB];
 #pragma unroll
-      for (int i = 0; i < NB; ++i) v[i] = acc[m][i][j];
-      if (part) store_row<float, NB>(part + r * T::edge_n, v, NB, true, false);
-      else if (r < p.M - m0) store_row<E, NB>(out + (long long)r * p.os, v, left, p.vec != 0, p.accumulate != 0);
+          for (int i = 0; i < NB; ++i) v[i] = pinned ? mfma_acc(acc[m][i], j) : acc[m][i][j];
+          put(m, j, v);
+        }
+  };
+  if (p.part) {
+    float* const part = p.part + ((long long)tile * p.pieces + piece) * (T::edge_m * T::edge_n) + (wm + kg * 4 * MB) * T::edge_n + wn + l16 * NB;
+    rows_out(0, MB, [&](int m, int j, const float (&v)[NB]) { store_row<float, NB>(part + (j * MB + m) * T::edge_n, v, false); });
+  } else if (p.vec && p.M - m0 >= T::edge_m && p.N - n0 >= T::edge_n) {
+    E* const out = static_cast<E*>(p.out) + (m0 + wm + kg * 4 * MB) * p.os + n0 + wn + l16 * NB;
+    rows_out(0, MB, [&](int m, int j, const float (&v)[NB]) { store_row<E, NB>(out + (j * MB + m) * p.os, v, p.accumulate != 0); });
+    if (!p.accumulate) {
+      // No load may reach LDS that is another workgroup's by then; stores may be under way still (a wave's memory operations
+      // count down in order), one for each of the rows.
+      product_wait<MB * 4>();
+      return;
     }
-  product_wait<0>();                                  // no load may reach LDS that is another workgroup's by then
+  } else {
+    // a tile on the edge, or rows that are not aligned: 64 rows of the wave tile at a time through LDS, value by value
+    constexpr int passes = MB / 4;
+    product_wait<0>();
+    meet();
+    float* const mine = reinterpret_cast<float*>(lds) + wave * (64 * T::wave_n);
+#pragma unroll
+    for (int h = 0; h < passes; ++h) {
+      rows_out(h * 4, 4, [&](int m, int j, const float (&v)[NB]) {
+        float* to = mine + ((kg * 4 + j) * 4 + m - h * 4) * T::wave_n + l16 * NB;
+#pragma unroll
+        for (int i = 0; i < NB; i += 4) *reinterpret_cast<float4*>(to + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+      });
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      const int below = p.M - m0 - wm, right = p.N - n0 - wn;
+      E* const out = static_cast<E*>(p.out) + (m0 + wm) * p.os + n0 + wn;
+#pragma unroll 1
+      for (int i = 0; i < 64; ++i) {
+        const int r = (i >> 2) * MB + h * 4 + (i & 3);
+        if (r >= below) continue;
+#pragma unroll
+        for (int c = 0; c < T::wave_n; c += 64)
+          if (c + lane < right) {
+            E* q = out + r * p.os + c + lane;
+            const float v = mine[i * T::wave_n + c + lane];
+            if constexpr (std::is_same<E, float>::value) *q = p.accumulate ? *q + v : v;
+            else *q = E(v);
+          }
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
+  }
+  product_wait<0>();
 }
 
 // Adds up the pieces of a split contraction in order: four columns of a tile row per lane.
@@ -506,8 +542,18 @@ template <int EDGE_M, int EDGE_N, typename E> __global__ __launch_bounds__(256) 
     v[2] += x.z;
     v[3] += x.w;
   }
-  store_row<E, 4>(static_cast<E*>(p.out) + (long long)(tm * EDGE_M + r) * p.os + tn * EDGE_N + c, v, p.N - tn * EDGE_N - c, p.vec != 0,
-                  p.accumulate != 0);
+  E* const out = static_cast<E*>(p.out) + (tm * EDGE_M + r) * p.os + tn * EDGE_N + c;
+  const int left = p.N - tn * EDGE_N - c;
+  if (p.vec && left >= 4) {
+    store_row<E, 4>(out, v, p.accumulate != 0);
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (i < left) {
+      if constexpr (std::is_same<E, float>::value) out[i] = p.accumulate ? out[i] + v[i] : v[i];
+      else out[i] = E(v[i]);
+    }
 }
 
 // ---------------------------------------------------------------------------------------------------------------------
@@ -628,7 +674,8 @@ template <typename E> hipError_t launch_product(const ProductArgs& p, bool large
 // of the best one on average.  Measured, few rows / small tiles / small tiles in 4 pieces / large: 3 x 5632 x 2048 7 / 11 / 11
 // / 23, 64 x 8192 x 8192 - / 29 / 20 / 60, 512 x 5632 x 2048 - / 15 / 26 / 35, 32768 x 5632 x 2048 - / 376 / - / 304 us.
 struct ProductChoice { int kernel, pieces; };          // kernel: 1 few rows, 4 small tiles, 8 large ones
-ProductChoice choose_product(long long M, long long N, int steps, bool fp32, int kernel, int pieces, bool split) {
+// Rows of the output that are not 16-byte aligned cost a large tile 12 us more, a small one 1.
+ProductChoice choose_product(long long M, long long N, int steps, bool fp32, bool aligned, int kernel, int pieces, bool split) {
   ProductChoice best{4, 1};
   double least = 1e300;
   auto offer = [&](int k, int n, double t) {
@@ -659,7 +706,7 @@ ProductChoice choose_product(long long M, long long N, int steps, bool fp32, int
         const double full = double((long long)w / (2 * kNumCu)), left = w - full * 2 * kNumCu;
         t = full * shared + (left > kNumCu ? shared : left > 0 ? alone : 0.0);
       } else {
-        t = double(((long long)w + kNumCu - 1) / kNumCu) * (s * 0.93 + 6.5);
+        t = double(((long long)w + kNumCu - 1) / kNumCu) * (s * 0.93 + (aligned || n > 1 ? 6.5 : 18.5));
       }
       offer(k, n, t + (n > 1 ? 1.7 + w * double(edge * edge) * 1e-6 : 0.0));
       if (n == steps) break;
@@ -781,10 +828,11 @@ extern "C" int adloco_block_product(adloco_ctx* ctx, const adloco_blocks8* a, co
   if (!scope.ok()) return fail(ctx, ADLOCO_EHIP, "block_product: device %d cannot be made current", ctx->device);
   hipStream_t st = static_cast<hipStream_t>(stream);
   const bool fp32 = dtype == ADLOCO_F32;
-  ProductChoice c = choose_product(a->rows, b->rows, p.steps, fp32, ctx->product_blocks, ctx->product_pieces, true);
+  const bool aligned = reinterpret_cast<uintptr_t>(out) % 16 == 0 && os * (int64_t)es % 16 == 0;
+  ProductChoice c = choose_product(a->rows, b->rows, p.steps, fp32, aligned, ctx->product_blocks, ctx->product_pieces, true);
   if (c.pieces > 1) {
     p.part = layer_scratch(ctx, st);
-    if (!p.part) c = choose_product(a->rows, b->rows, p.steps, fp32, ctx->product_blocks, ctx->product_pieces, false);
+    if (!p.part) c = choose_product(a->rows, b->rows, p.steps, fp32, aligned, ctx->product_blocks, ctx->product_pieces, false);
   }
   const bool few = c.kernel == 1, large = c.kernel == 8;
   const int64_t edge = large ? 256 : 128, tm = (a->rows + edge - 1) / edge, tn = (b->rows + edge - 1) / edge;
