@@ -203,10 +203,10 @@ __device__ __forceinline__ void tile_place(const ProductArgs& p, int tile, int& 
 }
 // Tile and piece of a workgroup: consecutive workgroups go to the eight XCDs in turn, each XCD gets a contiguous run of the
 // tiles, in bands of kTileGroup tile rows, so that what shares an L2 shares rows of A and columns of B.
-__device__ __forceinline__ bool product_place(const ProductArgs& p, int& tm, int& tn, int& piece, int& tile) {
+__device__ __forceinline__ bool product_place(const ProductArgs& p, int index, int& tm, int& tn, int& piece, int& tile) {
   const int tiles = p.tiles_m * p.tiles_n, total = tiles * p.pieces, per = (total + kNumXcd - 1) / kNumXcd;
-  const int w = (blockIdx.x % kNumXcd) * per + blockIdx.x / kNumXcd;
-  if (int(blockIdx.x / kNumXcd) >= per || w >= total) return false;
+  const int w = (index % kNumXcd) * per + index / kNumXcd;
+  if (index / kNumXcd >= per || w >= total) return false;
   tile = w / p.pieces;
   piece = w - tile * p.pieces;
   tile_place(p, tile, tm, tn);
@@ -239,9 +239,13 @@ __device__ __forceinline__ WideFrag widen(const mfma_i32x8& f, unsigned exponent
 // PINNED: accumulators in the accumulation registers and in assembly, for tiles that need all of them (the compiler moves
 // them about otherwise, and spills).  Operands and exponents come straight from LDS, so that no vector instruction that wrote
 // them stands near; fences as for mfma_16x16x32.
-template <int SEL_A, int SEL_B, bool PINNED>
+// FRESH: from zero, the old accumulators are only overwritten.
+template <int SEL_A, int SEL_B, bool PINNED, bool FRESH>
 __device__ __forceinline__ void scaled_mfma(mfma_f32x4& c, const mfma_i32x8& a, const mfma_i32x8& b, int ea, int eb) {
-  if constexpr (PINNED)
+  if constexpr (PINNED && FRESH)
+    asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, 0, %3, %4 op_sel:[%5,%6,0] op_sel_hi:[%7,%8,0]"
+                 : "=a"(c) : "v"(a), "v"(b), "v"(ea), "v"(eb), "n"(SEL_A & 1), "n"(SEL_B & 1), "n"(SEL_A >> 1), "n"(SEL_B >> 1));
+  else if constexpr (PINNED)
     asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[%5,%6,0] op_sel_hi:[%7,%8,0]"
                  : "+a"(c) : "v"(a), "v"(b), "v"(ea), "v"(eb), "n"(SEL_A & 1), "n"(SEL_B & 1), "n"(SEL_A >> 1), "n"(SEL_B >> 1));
   else
@@ -281,24 +285,27 @@ template <typename F, int... K> __device__ __forceinline__ void for_each_index(F
   (f(std::integral_constant<int, K>{}), ...);
 }
 
-template <int MB, int NB, bool EXACT, typename E>
+// WALK: one workgroup per compute unit takes tile after tile (every 32nd of its XCD's run), and asks for the first blocks of
+// the next one before it stores the outputs of this one, which then leave under its first products.  For whole contractions of
+// an even number of blocks.
+template <int MB, int NB, bool EXACT, bool WALK, typename E>
 __global__ __launch_bounds__(256, (TileShape<MB, NB, EXACT>::resident)) void product_tile_kernel(ProductArgs p) {
   using T = TileShape<MB, NB, EXACT>;
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
   int tm, tn, piece, tile;
-  if (!product_place(p, tm, tn, piece, tile)) return;
+  if (!product_place(p, blockIdx.x, tm, tn, piece, tile)) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l16 = lane & 15, kg = lane >> 4;
-  const int m0 = tm * T::edge_m, n0 = tn * T::edge_n;
+  int m0 = tm * T::edge_m, n0 = tn * T::edge_n;       // of the tile that is multiplied
   const int s0 = int((long long)p.steps * piece / p.pieces), n_steps = int((long long)p.steps * (piece + 1) / p.pieces) - s0;
   const unsigned at = lds_address(lds);
 
   // Direct loads of eight rows each.  Slot q of a wave tile holds its row (q % 16) * MB + q / 16 (the 16 rows of a block side
   // by side), chunk c of it at place c ^ (q / 2 % 8): the 16 lanes of a read
   // that go together lie in all 64 banks.  Rows behind the last one are the last one again.
-  const int chunk = ((lane & 7) ^ (lane >> 4)) * 16, last_a = p.M - m0 - 1, last_b = p.N - n0 - 1;
-  auto offset = [&](int tile_row, int q, int blocks, int last, long long stride) {
-    const int in = q + (lane >> 3), r = tile_row + (in & 15) * blocks + (in >> 4);
+  const int chunk = ((lane & 7) ^ (lane >> 4)) * 16;
+  auto offset = [&](int sub, int tile_row, int q, int blocks, int last, long long stride) {
+    const int in = q + sub, r = tile_row + (in & 15) * blocks + (in >> 4);
     return __umul24(unsigned(r < last ? r : last), unsigned(stride)) + (chunk ^ ((q & 8) * 8));
   };
   // A: load i of MB brings blocks of half i / (MB / 2) of both wave tiles' rows
@@ -312,21 +319,37 @@ __global__ __launch_bounds__(256, (TileShape<MB, NB, EXACT>::resident)) void pro
     t = u / (2 * NB);
     return (u % (2 * NB)) * 8;
   };
+  // exponents, four rows a lane; a wave brings 256 bytes of A's and B's (the four waves all of them, some twice)
+  const int e_at = (wave & 1) * (T::rows - 256) + lane * 4;
+  const bool of_b = e_at >= T::edge_m;
+  const int e_row = of_b ? e_at - T::edge_m : e_at;
+  const long long pe_step = of_b ? p.ebs : p.eas;
   unsigned off_a[MB], off_b[NB];
+  const unsigned char *base_a, *base_b, *pe;
+  int loaded = 0;
+  auto aim = [&](int tm, int tn) {                    // loads: to the first block of a tile
+    const int r0 = tm * T::edge_m, q0 = tn * T::edge_n, last_a = p.M - r0 - 1, last_b = p.N - q0 - 1;
+    int sub = lane >> 3;
+    if constexpr (WALK) asm volatile("" : "+v"(sub));   // (formed anew for every tile: kept, it costs registers that the loop needs)
 #pragma unroll
-  for (int i = 0; i < MB; ++i) {
-    int t;
-    const int q = slot_a(i, t);
-    off_a[i] = offset(t * T::wave_m, q, MB, last_a, p.as);
-  }
+    for (int i = 0; i < MB; ++i) {
+      int t;
+      const int q = slot_a(i, t);
+      off_a[i] = offset(sub, t * T::wave_m, q, MB, last_a, p.as);
+    }
 #pragma unroll
-  for (int i = 0; i < NB; ++i) {
-    int t;
-    const int q = slot_b(i, t);
-    off_b[i] = offset(t * T::wave_n, q, NB, last_b, p.bs);
-  }
-  const unsigned char* base_a = uniform_ptr(p.a + (long long)m0 * p.as + (long long)s0 * 128);
-  const unsigned char* base_b = uniform_ptr(p.b + (long long)n0 * p.bs + (long long)s0 * 128);
+    for (int i = 0; i < NB; ++i) {
+      int t;
+      const int q = slot_b(i, t);
+      off_b[i] = offset(sub, t * T::wave_n, q, NB, last_b, p.bs);
+    }
+    base_a = uniform_ptr(p.a + (long long)r0 * p.as + (long long)s0 * 128);
+    base_b = uniform_ptr(p.b + (long long)q0 * p.bs + (long long)s0 * 128);
+    const int e_rows = of_b ? p.N - q0 : p.M - r0;
+    pe = (of_b ? p.eb + (long long)s0 * p.ebs + q0 : p.ea + (long long)s0 * p.eas + r0) + (e_row < e_rows ? e_row : 0);
+    loaded = 0;
+  };
+  aim(tm, tn);
   auto load_a = [&](int buf, int i) {
     int t;
     const int q = slot_a(i, t);
@@ -337,13 +360,6 @@ __global__ __launch_bounds__(256, (TileShape<MB, NB, EXACT>::resident)) void pro
     const int q = slot_b(i, t);
     direct_load_lds16_s(off_b[i], base_b, at + buf * T::stage + (T::edge_m + t * T::wave_n + q) * 128);
   };
-  // exponents, four rows a lane; a wave brings 256 bytes of A's and B's (the four waves all of them, some twice)
-  const int e_at = (wave & 1) * (T::rows - 256) + lane * 4;
-  const bool of_b = e_at >= T::edge_m;
-  const int e_row = of_b ? e_at - T::edge_m : e_at, e_rows = of_b ? p.N - n0 : p.M - m0;
-  const unsigned char* pe = (of_b ? p.eb + (long long)s0 * p.ebs + n0 : p.ea + (long long)s0 * p.eas + m0) + (e_row < e_rows ? e_row : 0);
-  const long long pe_step = of_b ? p.ebs : p.eas;
-  int loaded = 0;
   auto load_first = [&](int buf, int i) {             // item i of first_loads
     if (i == 0) {
       direct_load_lds4(pe, at + buf * T::stage + T::rows * 128 + (wave & 1) * (T::rows - 256));
@@ -377,8 +393,14 @@ __global__ __launch_bounds__(256, (TileShape<MB, NB, EXACT>::resident)) void pro
 
   constexpr bool pinned = MB * NB == 64 && !EXACT;
   constexpr int ahead = T::ahead;
-  mfma_f32x4 acc[MB][NB] = {};
-  if constexpr (pinned) mfma_fence(acc);
+  mfma_f32x4 acc[MB][NB];
+  if constexpr (!WALK) {
+#pragma unroll
+    for (int m = 0; m < MB; ++m)
+#pragma unroll
+      for (int n = 0; n < NB; ++n) acc[m][n] = mfma_f32x4{0.f, 0.f, 0.f, 0.f};
+    if constexpr (pinned) mfma_fence(acc);
+  }
   struct Held { mfma_i32x8 b[NB], a[ahead]; int ea[MB / 4], eb[NB / 4]; };
   constexpr int fetches = 1 + ahead + NB;
   auto fetch = [&](int buf, Held& h, int i) {         // item i of fetches
@@ -401,7 +423,14 @@ __global__ __launch_bounds__(256, (TileShape<MB, NB, EXACT>::resident)) void pro
   // fetched like any other (the last one again, into places that nobody reads any more), so that all steps are alike.
   // A wave issues in order, and a matrix instruction keeps the matrix core busy for eight issue slots: loads and LDS reads are
   // dealt out one by one between them.
-  auto step = [&](int buf, Held& h, Held& next) {
+  // FRESH: the first block of a walked tile, whose products overwrite the accumulators.  behind_1, behind_2: stores of the
+  // tile before that lie between the loads that are waited for and the wait (memory operations of a wave count down in order).
+  constexpr int stores = MB * 4;
+  auto wait = [](bool behind) {
+    if (WALK && behind) product_wait<T::first_loads + T::second_loads + stores>();
+    else product_wait<T::first_loads + T::second_loads>();
+  };
+  auto step = [&](auto fresh, int buf, Held& h, Held& next, bool behind_1, bool behind_2) {
     constexpr int meet_1 = (MB / 2 - ahead) * NB, meet_2 = (MB - ahead) * NB, end = MB * NB;
     mfma_i32x8 a[MB];
 #pragma unroll
@@ -410,11 +439,11 @@ __global__ __launch_bounds__(256, (TileShape<MB, NB, EXACT>::resident)) void pro
     auto slot = [&](auto index) {
       constexpr int k = decltype(index)::value, m = k / NB, n = k % NB;
       if constexpr (k == meet_1) {                    // B and the first half of A have been read; the second half is needed
-        product_wait<T::first_loads + T::second_loads>();
+        wait(behind_1);
         meet();
       }
       if constexpr (k == meet_2) {                    // all of A has been read; the next block's first part is needed
-        product_wait<T::first_loads + T::second_loads>();
+        wait(behind_2);
         meet();
       }
       if constexpr (EXACT) {
@@ -423,7 +452,7 @@ __global__ __launch_bounds__(256, (TileShape<MB, NB, EXACT>::resident)) void pro
 #pragma unroll
         for (int x = 0; x < 4; ++x) acc[m][n] = mfma_16x16x32_v<false>(wa.k[x], wb[n].k[x], acc[m][n]);
       } else {
-        scaled_mfma<(m & 3), (n & 3), pinned>(acc[m][n], a[m], h.b[n], h.ea[m / 4], h.eb[n / 4]);
+        scaled_mfma<(m & 3), (n & 3), pinned, decltype(fresh)::value>(acc[m][n], a[m], h.b[n], h.ea[m / 4], h.eb[n / 4]);
       }
       if constexpr (n == 0 && m + ahead < MB) a[m + ahead] = frag(buf, row_a, m + ahead);
       if constexpr (k >= meet_1 && k < meet_2) {
@@ -449,20 +478,6 @@ __global__ __launch_bounds__(256, (TileShape<MB, NB, EXACT>::resident)) void pro
 #pragma unroll
     for (int i = 0; i < T::second_loads; ++i) load_second(buf, i);
   };
-  load(0);
-  load(1);
-  product_wait<T::first_loads + 2 * T::second_loads>();
-  meet();
-  Held h0, h1;
-#pragma unroll
-  for (int i = 0; i < fetches; ++i) fetch(0, h0, i);
-  for (int s = 0; s + 1 < n_steps; s += 2) {
-    step(0, h0, h1);
-    step(1, h1, h0);
-  }
-  if (n_steps & 1) step(0, h0, h1);
-
-  if constexpr (pinned) mfma_fence(acc);
   // Element j of block (m, n): row (kg * 4 + j) * MB + m of the wave tile, column l16 * NB + n.  Three ways out, each short
   // enough for the instruction cache (checks woven into one of them: 60 KB of code, 4 us a tile).
   auto rows_out = [&](int first, int count, auto put) {
@@ -477,51 +492,107 @@ __global__ __launch_bounds__(256, (TileShape<MB, NB, EXACT>::resident)) void pro
           put(m, j, v);
         }
   };
-  if (p.part) {
-    float* const part = p.part + ((long long)tile * p.pieces + piece) * (T::edge_m * T::edge_n) + (wm + kg * 4 * MB) * T::edge_n + wn + l16 * NB;
-    rows_out(0, MB, [&](int m, int j, const float (&v)[NB]) { store_row<float, NB>(part + (j * MB + m) * T::edge_n, v, false); });
-  } else if (p.vec && p.M - m0 >= T::edge_m && p.N - n0 >= T::edge_n) {
-    E* const out = static_cast<E*>(p.out) + (m0 + wm + kg * 4 * MB) * p.os + n0 + wn + l16 * NB;
-    rows_out(0, MB, [&](int m, int j, const float (&v)[NB]) { store_row<E, NB>(out + (j * MB + m) * p.os, v, p.accumulate != 0); });
-    if (!p.accumulate) {
-      // No load may reach LDS that is another workgroup's by then; stores may be under way still (a wave's memory operations
-      // count down in order), one for each of the rows.
-      product_wait<MB * 4>();
-      return;
+  auto store = [&]() -> bool {                        // true: by `stores` memory operations, and nothing else of LDS
+    if constexpr (pinned) mfma_fence(acc);
+    int row0 = wm + kg * 4 * MB;
+    if constexpr (WALK) asm volatile("" : "+v"(row0));
+    if (p.part) {
+      float* const part = p.part + ((long long)tile * p.pieces + piece) * (T::edge_m * T::edge_n) + row0 * T::edge_n + wn + l16 * NB;
+      rows_out(0, MB, [&](int m, int j, const float (&v)[NB]) { store_row<float, NB>(part + (j * MB + m) * T::edge_n, v, false); });
+    } else if (p.vec && p.M - m0 >= T::edge_m && p.N - n0 >= T::edge_n) {
+      E* const out = static_cast<E*>(p.out) + (m0 + row0) * p.os + n0 + wn + l16 * NB;
+      rows_out(0, MB, [&](int m, int j, const float (&v)[NB]) { store_row<E, NB>(out + (j * MB + m) * p.os, v, p.accumulate != 0); });
+      return !p.accumulate;
+    } else {
+      // a tile on the edge, or rows that are not aligned: 64 rows of the wave tile at a time through LDS, value by value
+      constexpr int passes = MB / 4;
+      product_wait<0>();
+      meet();
+      float* const mine = reinterpret_cast<float*>(lds) + wave * (64 * T::wave_n);
+#pragma unroll
+      for (int h = 0; h < passes; ++h) {
+        rows_out(h * 4, 4, [&](int m, int j, const float (&v)[NB]) {
+          float* to = mine + ((kg * 4 + j) * 4 + m - h * 4) * T::wave_n + l16 * NB;
+#pragma unroll
+          for (int i = 0; i < NB; i += 4) *reinterpret_cast<float4*>(to + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+        });
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        const int below = p.M - m0 - wm, right = p.N - n0 - wn;
+        E* const out = static_cast<E*>(p.out) + (m0 + wm) * p.os + n0 + wn;
+#pragma unroll 1
+        for (int i = 0; i < 64; ++i) {
+          const int r = (i >> 2) * MB + h * 4 + (i & 3);
+          if (r >= below) continue;
+#pragma unroll
+          for (int c = 0; c < T::wave_n; c += 64)
+            if (c + lane < right) {
+              E* q = out + r * p.os + c + lane;
+              const float v = mine[i * T::wave_n + c + lane];
+              if constexpr (std::is_same<E, float>::value) *q = p.accumulate ? *q + v : v;
+              else *q = E(v);
+            }
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      }
+    }
+    return false;
+  };
+  Held h0, h1;
+  auto begin = [&](bool behind) {                     // the first block is here: fetch what its first products take
+    if (WALK && behind) product_wait<T::first_loads + 2 * T::second_loads + stores>();
+    else product_wait<T::first_loads + 2 * T::second_loads>();
+    meet();
+#pragma unroll
+    for (int i = 0; i < fetches; ++i) fetch(0, h0, i);
+  };
+  constexpr std::integral_constant<bool, false> more{};
+  load(0);
+  load(1);
+  bool behind = false;
+  if constexpr (WALK) {
+    constexpr std::integral_constant<bool, true> fresh{};
+    for (int w = blockIdx.x;;) {
+      begin(behind);
+      step(fresh, 0, h0, h1, behind, behind);
+      step(more, 1, h1, h0, behind, false);
+#pragma unroll 1
+      for (int s = 2; s < n_steps; s += 2) {
+        step(more, 0, h0, h1, false, false);
+        step(more, 1, h1, h0, false, false);
+      }
+      w += kNumCu;
+      const bool on = product_place(p, w, tm, tn, piece, tile);
+      const bool plain = p.vec && p.M - m0 >= T::edge_m && p.N - n0 >= T::edge_n;
+      product_wait<0>();                              // (the last loads went to the places that the next ones take)
+      if (on && plain) {
+        aim(tm, tn);
+        load(0);
+        load(1);
+      }
+      behind = store();
+      if (!on) break;
+      m0 = tm * T::edge_m;
+      n0 = tn * T::edge_n;
+      if (!plain) {                                   // (LDS served the outputs)
+        meet();
+        aim(tm, tn);
+        load(0);
+        load(1);
+      }
     }
   } else {
-    // a tile on the edge, or rows that are not aligned: 64 rows of the wave tile at a time through LDS, value by value
-    constexpr int passes = MB / 4;
-    product_wait<0>();
-    meet();
-    float* const mine = reinterpret_cast<float*>(lds) + wave * (64 * T::wave_n);
-#pragma unroll
-    for (int h = 0; h < passes; ++h) {
-      rows_out(h * 4, 4, [&](int m, int j, const float (&v)[NB]) {
-        float* to = mine + ((kg * 4 + j) * 4 + m - h * 4) * T::wave_n + l16 * NB;
-#pragma unroll
-        for (int i = 0; i < NB; i += 4) *reinterpret_cast<float4*>(to + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
-      });
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      const int below = p.M - m0 - wm, right = p.N - n0 - wn;
-      E* const out = static_cast<E*>(p.out) + (m0 + wm) * p.os + n0 + wn;
-#pragma unroll 1
-      for (int i = 0; i < 64; ++i) {
-        const int r = (i >> 2) * MB + h * 4 + (i & 3);
-        if (r >= below) continue;
-#pragma unroll
-        for (int c = 0; c < T::wave_n; c += 64)
-          if (c + lane < right) {
-            E* q = out + r * p.os + c + lane;
-            const float v = mine[i * T::wave_n + c + lane];
-            if constexpr (std::is_same<E, float>::value) *q = p.accumulate ? *q + v : v;
-            else *q = E(v);
-          }
-      }
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    begin(false);
+    for (int s = 0; s + 1 < n_steps; s += 2) {
+      step(more, 0, h0, h1, false, false);
+      step(more, 1, h1, h0, false, false);
     }
+    if (n_steps & 1) step(more, 0, h0, h1, false, false);
+    behind = store();
   }
-  product_wait<0>();
+  // No load may reach LDS that is another workgroup's by then; stores may be under way still (a wave's memory operations
+  // count down in order).
+  if (behind) product_wait<stores>();
+  else product_wait<0>();
 }
 
 // Adds up the pieces of a split contraction in order: four columns of a tile row per lane.
@@ -609,7 +680,7 @@ template <int RB, int WAVES, bool EXACT, typename E> __global__ __launch_bounds_
 #pragma unroll
           for (int k = 0; k < 4; ++k) acc[r] = mfma_16x16x32_v<false>(wa.k[k], wb.k[k], acc[r]);
         } else {
-          scaled_mfma<0, 0, false>(acc[r], fa[i][r], fb[i], xa[i][r], xb[i]);
+          scaled_mfma<0, 0, false, false>(acc[r], fa[i][r], fb[i], xa[i][r], xb[i]);
         }
       }
     }
@@ -637,14 +708,15 @@ template <typename E, bool FAST> hipError_t launch_pack(const PackArgs& a, unsig
   hipLaunchKernelGGL((pack_blocks_kernel<E, FAST>), dim3(blocks), dim3(kPackThreads), 0, st, a);
   return hipGetLastError();
 }
-template <int MB, int NB, typename E> hipError_t launch_tiles(const ProductArgs& p, hipStream_t st) {
+template <int MB, int NB, bool WALK, typename E> hipError_t launch_tiles(const ProductArgs& p, hipStream_t st) {
   constexpr bool exact = std::is_same<E, float>::value;
   using T = TileShape<MB, NB, exact>;
-  auto kern = product_tile_kernel<MB, NB, exact, E>;
+  auto kern = product_tile_kernel<MB, NB, exact, WALK, E>;
   const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, T::lds);
   if (e != hipSuccess) return e;
   const unsigned total = unsigned(p.tiles_m) * unsigned(p.tiles_n);
-  hipLaunchKernelGGL(kern, dim3((total * p.pieces + kNumXcd - 1) / kNumXcd * kNumXcd), dim3(256), T::lds, st, p);
+  const unsigned groups = WALK ? kNumCu : (total * p.pieces + kNumXcd - 1) / kNumXcd * kNumXcd;
+  hipLaunchKernelGGL(kern, dim3(groups), dim3(256), T::lds, st, p);
   if (p.part)
     hipLaunchKernelGGL((product_join_kernel<T::edge_m, T::edge_n, E>), dim3(total * (T::edge_m * T::edge_n / 1024)), dim3(256), 0, st, p);
   return hipGetLastError();
@@ -661,10 +733,15 @@ template <int RB, typename E> hipError_t launch_few_rows(const ProductArgs& p, h
 template <typename E> hipError_t launch_few(const ProductArgs& p, hipStream_t st) {
   return p.M <= 16 ? launch_few_rows<1, E>(p, st) : launch_few_rows<2, E>(p, st);
 }
+// More large tiles than compute units, whole, of an even number of blocks: one workgroup per compute unit walks over them (one
+// workgroup per tile / walking: 32768 x 5632 x 2048 357 / 342 us, x 512 118 / 114, 8192 x 8192 x 1024 66 / 64).
 template <typename E> hipError_t launch_product(const ProductArgs& p, bool large, hipStream_t st) {
   if constexpr (!std::is_same<E, float>::value)
-    if (large) return launch_tiles<8, 8, E>(p, st);
-  return launch_tiles<4, 4, E>(p, st);
+    if (large) {
+      const bool walk = p.pieces == 1 && p.steps % 2 == 0 && p.tiles_m * p.tiles_n > kNumCu;
+      return walk ? launch_tiles<8, 8, true, E>(p, st) : launch_tiles<8, 8, false, E>(p, st);
+    }
+  return launch_tiles<4, 4, false, E>(p, st);
 }
 
 // Which kernel, and how many pieces the contraction is cut into.  Times in microseconds, fitted to 5600 timings over 250
@@ -672,9 +749,9 @@ template <typename E> hipError_t launch_product(const ProductArgs& p, bool large
 // that has its compute unit to itself and 0.95 for two that share it (fp32 outputs 0.75 and 1.5), 0.93 for a large tile, 3.0
 // and 6.5 to start and store one; 1.7 and the partial tiles' way out and back for a second kernel.  The choice is within 4 %
 // of the best one on average.  Measured, few rows / small tiles / small tiles in 4 pieces / large: 3 x 5632 x 2048 7 / 11 / 11
-// / 23, 64 x 8192 x 8192 - / 29 / 20 / 60, 512 x 5632 x 2048 - / 15 / 26 / 35, 32768 x 5632 x 2048 - / 376 / - / 304 us.
+// / 23, 64 x 8192 x 8192 - / 29 / 20 / 60, 512 x 5632 x 2048 - / 15 / 26 / 35, 32768 x 5632 x 2048 - / 376 / - / 300 us.
+// Rows of the output that are not 16-byte aligned cost a large tile 12 us more, a small one 1 (32001 x 2044 x 1024: 82 / 124).
 struct ProductChoice { int kernel, pieces; };          // kernel: 1 few rows, 4 small tiles, 8 large ones
-// Rows of the output that are not 16-byte aligned cost a large tile 12 us more, a small one 1.
 ProductChoice choose_product(long long M, long long N, int steps, bool fp32, bool aligned, int kernel, int pieces, bool split) {
   ProductChoice best{4, 1};
   double least = 1e300;

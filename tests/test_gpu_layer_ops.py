@@ -257,6 +257,24 @@ def test_block_product(ctx, variant, m, n, k, dtype):
     assert bool((buf == 7).all())
 
 
+@pytest.mark.parametrize("pad", [0, 4, 1])             # rows of the output: 16-byte aligned, 8, 2
+@pytest.mark.parametrize("m,n,k", [(4352, 4096, 250), (4352, 4096, 900), (4200, 4100, 1024), (65281, 256, 512), (250, 131000, 256)])
+def test_block_product_of_more_large_tiles_than_compute_units(ctx, m, n, k, pad):
+    """Whole numbers again, against the product in 64 bits on the device; every tile is written once, nothing between the rows."""
+    a, b = random_blocks(m, m, k, True)[0], random_blocks(n, n, k, True)[0]
+    av, bv = (x.data[:, :k].view(torch.float8_e4m3fn).double() for x in (a, b))
+    want = av @ bv.T.contiguous()
+    ctx.set_tuning("product_blocks", 8)
+    try:
+        for dt in (torch.bfloat16, torch.float16):
+            buf = torch.full((m, n + pad), 7.0, dtype=dt, device=DEV)
+            A.adloco_block_product(ctx, a, b, buf[:, :n])
+            assert torch.equal(buf[:, :n], want.to(dt))
+            assert bool((buf[:, n:] == 7).all())
+    finally:
+        ctx.set_tuning("product_blocks", 0)
+
+
 def test_block_product_of_sliced_operands(ctx, variant):
     (a, av), (b, bv) = random_blocks(1, 96, 640, True), random_blocks(2, 80, 640, True)
     sa = A.Blocks8(a.data[16:], a.exponent[:, 16:], 70, 640)            # rows 16 .. 85
