@@ -317,6 +317,8 @@ def make_layer_descs(layers: Sequence[dict], B: int, T: int, dtype: int):
             if not d.is_cuda or d.dtype != torch.float32 or d.dim() != 2 or d.shape[0] != B or d.stride(1) != 1:
                 raise ValueError(f"layer {i}: sums must be a GPU fp32 tensor [B={B},d] with unit stride in d, got "
                                  f"{tuple(d.shape)} {d.dtype}")
+            if B > 1 and d.stride(0) < d.shape[1]:        # (0, of an expanded tensor, would stand for d_out)
+                raise ValueError(f"layer {i}: rows of sums must not share memory")
             d = d.unsqueeze(1)
         else:
             d = l["delta"]

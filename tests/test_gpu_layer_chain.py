@@ -109,6 +109,13 @@ def test_sample_sums_refusals(ctx):
         A.make_layer_descs([dict(kind="sample_sums", sums=sums.bfloat16(), grad_sum=g)], B, T, A.ADLOCO_BF16)
 
 
+def test_expanded_sample_sums_are_refused(ctx):
+    one, g = torch.zeros(8, device=DEV), torch.zeros(8, device=DEV)
+    for sums in (one.expand(4, 8), torch.zeros(32, device=DEV).as_strided((4, 8), (4, 1))):
+        with pytest.raises(ValueError, match="share memory"):
+            A.make_layer_descs([dict(kind="sample_sums", sums=sums, grad_sum=g)], 4, 3, A.ADLOCO_BF16)
+
+
 def test_round_takes_sample_sums(ctx):
     """adloco_round with a block given by its per-sample sums: the same bits as with the tokens' gradients (whole numbers)."""
     T, d, N = 5, 40, 40 + 8 * 16
