@@ -13,10 +13,11 @@ const char* check_blocks8(const adloco_blocks8* b) {
   if (b->rows > 0 && (!b->data || !b->exponent)) return "data or exponent is NULL";
   if (reinterpret_cast<uintptr_t>(b->data) % 16 || reinterpret_cast<uintptr_t>(b->exponent) % 16)
     return "data and exponent must be 16-byte aligned";
-  if (b->row_stride < wide || b->row_stride % 16 || b->row_stride > (int64_t(1) << 40))
-    return "row_stride must hold whole blocks of 128 and be a multiple of 16";
-  if (b->exponent_stride < b->rows || b->exponent_stride % 16 || b->exponent_stride > (int64_t(1) << 40))
-    return "exponent_stride must be a multiple of 16 and at least rows";
+  if (b->row_stride < wide || b->row_stride % 16 || b->row_stride > (int64_t(1) << 40) || !span_in_reach(b->rows, b->row_stride))
+    return "row_stride must hold whole blocks of 128, be a multiple of 16 and within reach";
+  if (b->exponent_stride < b->rows || b->exponent_stride % 16 || b->exponent_stride > (int64_t(1) << 40) ||
+      !span_in_reach(wide / 128, b->exponent_stride))
+    return "exponent_stride must be a multiple of 16, at least rows and within reach";
   return nullptr;
 }
 
@@ -822,7 +823,7 @@ extern "C" int adloco_pack_blocks(adloco_ctx* ctx, const void* x, int64_t x_row_
   }
   const size_t es = size_of(dtype);
   const int64_t xs = x_row_stride ? x_row_stride : cols;
-  if (!x || xs < cols || xs > (int64_t(1) << 40) || reinterpret_cast<uintptr_t>(x) % es)
+  if (!x || xs < cols || xs > (int64_t(1) << 40) || !span_in_reach(rows, xs * (int64_t)es) || reinterpret_cast<uintptr_t>(x) % es)
     return fail(ctx, ADLOCO_EINVAL, "pack_blocks: x is NULL or misaligned, or its row stride is smaller than the row or out of range");
   const RowSpan s[5] = {{x, rows, (long long)(cols * es), (long long)(xs * es)}, values_of(along), exponents_of(along),
                         values_of(across), exponents_of(across)};
@@ -878,7 +879,8 @@ extern "C" int adloco_block_product(adloco_ctx* ctx, const adloco_blocks8* a, co
   if (a->rows == 0 || b->rows == 0) return ADLOCO_OK;
   const size_t es = size_of(dtype);
   const int64_t os = out_row_stride ? out_row_stride : b->rows;
-  if (!out || os < b->rows || os > (int64_t(1) << 40) || reinterpret_cast<uintptr_t>(out) % es)
+  if (!out || os < b->rows || os > (int64_t(1) << 40) || !span_in_reach(a->rows, os * (int64_t)es) ||
+      reinterpret_cast<uintptr_t>(out) % es)
     return fail(ctx, ADLOCO_EINVAL, "block_product: out is NULL or misaligned, or its row stride is smaller than the row or out of range");
   const RowSpan so{out, a->rows, (long long)(b->rows * es), (long long)(os * es)};
   for (const adloco_blocks8* x : {a, b})

@@ -342,7 +342,7 @@ bool check_matrices(adloco_ctx* ctx, const char* who, Matrix* m, int n, int64_t 
   for (int i = 0; i < n; ++i) {
     if (m[i].stride == 0) m[i].stride = d;
     if (!m[i].p) continue;
-    if (m[i].stride < d || m[i].stride > (int64_t(1) << 40)) {
+    if (m[i].stride < d || m[i].stride > (int64_t(1) << 40) || !span_in_reach(rows, m[i].stride * (int64_t)es)) {
       fail(ctx, ADLOCO_EINVAL, "%s: row stride of %s is smaller than the row or out of range", who, m[i].name);
       return false;
     }
@@ -483,7 +483,8 @@ extern "C" int adloco_rms_norm(adloco_ctx* ctx, const adloco_norm_io* io, int64_
     if (spans_overlap(s, q) || spans_overlap(s, ex) || (x.written && spans_overlap(s, gain)))
       return fail(ctx, ADLOCO_EINVAL, "rms_norm: %s overlaps y8 or gain", x.name);
   }
-  if (spans_overlap(gain, q) || spans_overlap(gain, ex)) return fail(ctx, ADLOCO_EINVAL, "rms_norm: gain overlaps y8");
+  if (spans_overlap(gain, q) || spans_overlap(gain, ex) || spans_overlap(q, ex))
+    return fail(ctx, ADLOCO_EINVAL, "rms_norm: y8 overlaps gain or itself");
   a.x = io->x;
   a.residual = io->residual;
   a.gain = io->gain;

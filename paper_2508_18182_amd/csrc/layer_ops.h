@@ -220,6 +220,8 @@ struct RowSpan {
   long long rows, width, stride;
   bool same(const RowSpan& o) const { return p == o.p && (stride == o.stride || rows <= 1); }
 };
+// Whether its size fits the arithmetic of addresses.
+inline bool span_in_reach(long long rows, long long stride) { return rows <= 1 || stride <= (1LL << 56) / rows; }
 // Whether two of them may share a byte.  Column ranges of one buffer (equal strides) do not.
 inline bool spans_overlap(const RowSpan& x, const RowSpan& y) {
   if (!x.p || !y.p || x.rows <= 0 || y.rows <= 0) return false;

@@ -220,6 +220,29 @@ def test_rms_norm_backward_refuses(host, io, change, want):
                  a["eps"], a["mask"], None) == want
 
 
+def test_strides_beyond_all_memory_are_refused(host):
+    """Rows times stride beyond 64 bits: the check for overlaps would be made on what is left of the product."""
+    far, many = 1 << 40, 1 << 30
+    assert _code(host, "adloco_dropout", BASE, far, None, 0, BASE, far, many, 64, A.ADLOCO_F32, _mask(), None) == EINVAL
+    io = _io(bind.NormIo, residual=None, h=None, x_row_stride=far, y_row_stride=far)
+    assert _code(host, "adloco_rms_norm", C.byref(io), many, 64, A.ADLOCO_F32, 1e-5, None, None, None) == EINVAL
+    io = _io(bind.NormBackwardIo, dh_row_stride=far)
+    assert _code(host, "adloco_rms_norm_backward", C.byref(io), 1, many, 64, A.ADLOCO_F32, 1e-5, None, None) == EINVAL
+    wide, tall = _blocks(rows=many, row_stride=far, exponent_stride=many), _blocks(cols=many, row_stride=many, exponent_stride=far)
+    small = _blocks(data=BASE + (1 << 50), exponent=BASE + (1 << 51))
+    for b in (wide, tall):
+        assert _code(host, "adloco_pack_blocks", BASE, 0, b.rows, b.cols, A.ADLOCO_F32, b, None, None) == EINVAL
+        assert _code(host, "adloco_block_product", b, b, BASE, 0, A.ADLOCO_F32, 0, None) == EINVAL
+    assert _code(host, "adloco_pack_blocks", BASE, far, many, 256, A.ADLOCO_F32, _blocks(rows=many, exponent_stride=many), None, None) == EINVAL
+    assert _code(host, "adloco_block_product", _blocks(rows=many, exponent_stride=many), small, BASE, far, A.ADLOCO_F32, 0, None) == EINVAL
+
+
+def test_rms_norm_refuses_blocks_that_overlap_themselves(host):
+    y8 = _blocks(rows=8, cols=64, row_stride=128, exponent_stride=16, exponent=BASE + 16)
+    io = _io(bind.NormIo)
+    assert _code(host, "adloco_rms_norm", C.byref(io), 8, 64, A.ADLOCO_BF16, 1e-5, None, y8, None) == EINVAL
+
+
 def test_binding_refuses_before_the_library():
     class Ctx:
         device, _h = 0, None
