@@ -275,6 +275,30 @@ def test_block_product_of_more_large_tiles_than_compute_units(ctx, m, n, k, pad)
         ctx.set_tuning("product_blocks", 0)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("ea,eb,top", [(0, 200, 448), (1, 200, 448), (2, 230, 448), (3, 200, 448), (200, 1, 448), (246, 60, 448),
+                                       (60, 246, 448), (247, 60, 240), (254, 20, 1.75), (3, 246, 448), (255, 127, 448)])
+def test_block_product_of_extreme_exponents(ctx, variant, ea, eb, top, dtype):
+    dt, m, n, k = TYPES[dtype], 70, 48, 200
+    r = np.random.default_rng(ea + eb)
+    (a, _), (b, _) = random_blocks(1, m, k), random_blocks(2, n, k)
+    every = torch.arange(256, dtype=torch.uint8).view(torch.float8_e4m3fn).double()
+    codes = torch.nonzero(every.abs() <= top).flatten().to(torch.uint8)        # (NaN compares false)
+    ca, cb = (codes[torch.from_numpy(r.integers(0, len(codes), s))] for s in ((m, k), (n, k)))
+    a.data[:, :k], b.data[:, :k] = ca.to(DEV), cb.to(DEV)
+    a.exponent[:, :m], b.exponent[:, :n] = ea, eb
+    av, bv = (host(c.view(torch.float8_e4m3fn).double()) * 2.0**(e - 127) for c, e in ((ca, ea), (cb, eb)))
+    want, size = av @ bv.T, np.abs(av) @ np.abs(bv).T
+    out = torch.empty(m, n, dtype=dt, device=DEV)
+    A.adloco_block_product(ctx, a, b, out)
+    if ea == 255:
+        assert bool(out.isnan().all())
+        return
+    lost = 2.0**-134 * ((ea < 3) * np.abs(bv).sum(1)[None] + (eb < 3) * np.abs(av).sum(1)[:, None])      # operands below 2^-133
+    cut = lost + 2 * k * U * size if dtype == "f32" else (2.0**-13 * 32 + 2 * k * U) * size
+    close(out, want, half(dt) * np.abs(want) + cut * (1 + half(dt)) + tiny(dt))
+
+
 def test_block_product_of_sliced_operands(ctx, variant):
     (a, av), (b, bv) = random_blocks(1, 96, 640, True), random_blocks(2, 80, 640, True)
     sa = A.Blocks8(a.data[16:], a.exponent[:, 16:], 70, 640)            # rows 16 .. 85
