@@ -26,7 +26,8 @@ namespace {
 // ---------------------------------------------------------------------------------------------------------------------
 // Packing.  A workgroup of eight waves takes 128 x 128 values, a lane eight columns of four rows in registers: blocks along
 // the rows are 16 lanes of a row, blocks across them the 32 groups of four rows.  x is read once whichever of the two outputs
-// are asked for; the transposed one goes through LDS, so that both are stored in whole lines.
+// are asked for; the transposed one goes through LDS, so that both are stored in whole lines.  Bound by memory and by the two
+// trips through a workgroup (load, reduce, turn, store): 32768 x 1024 bf16 both ways 25 us, 5.4 TB/s; 5632 x 2048 fp32 16 us.
 // ---------------------------------------------------------------------------------------------------------------------
 struct PackArgs {
   const void* x;
@@ -178,6 +179,9 @@ template <typename E, bool FAST> __global__ __launch_bounds__(kPackThreads) void
 // have to be under way all the time: the workgroup meets twice per block and refills in two parts whatever has been read --
 // after the first half of A's blocks their place and B's, after the second half theirs -- which gives every load one and a
 // half blocks of time until it is needed, out of two stages.
+//   Measured: 32768 x 5632 x 2048 to bf16 291 us, 2.6 PFLOP/s; 8192^3 375 us, 2.9; 16384^3 2.69 ms, 3.3.  fp32 out: 8192^3 815 us,
+// 1.35 PFLOP/s; 1024 x 4096 x 32033 228 us, 1.2.  The matrix cores are busy for 73 % and 56 % of the cycles (and the clock falls
+// to 1.7 and 1.9 GHz under them); in the second, widening takes as many vector cycles as the products take matrix cycles.
 // ---------------------------------------------------------------------------------------------------------------------
 typedef __attribute__((ext_vector_type(8))) int mfma_i32x8;
 typedef __attribute__((ext_vector_type(4))) int i32x4;
@@ -631,6 +635,7 @@ template <int EDGE_M, int EDGE_N, typename E> __global__ __launch_bounds__(256) 
 // ---------------------------------------------------------------------------------------------------------------------
 // Few rows of A (up to 32): B is read once, by whoever multiplies it, straight into registers; all else is latency.  A
 // workgroup takes 16 columns, its waves share the blocks of k among them and add up what they have through LDS, in order.
+// 3 x 5632 x 2048: 5.2 us (on small tiles 11), 2.2 TB/s of B; 33 to 64 rows would take 13 us, on small tiles 10.
 // ---------------------------------------------------------------------------------------------------------------------
 constexpr int kFewRows = 32;
 

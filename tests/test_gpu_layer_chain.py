@@ -261,6 +261,25 @@ def test_step_in_a_graph_and_on_other_streams():
     ctx.close()
 
 
+def test_without_memory_for_scratch():
+    """Sums that would be split are taken whole, eagerly too, and split once there is memory: whole numbers, the same bits."""
+    ctx = A.Context(0)
+    ctx.set_tuning("scratch_limit_kb", 1)
+    a, b = A.Blocks8.empty(64, 20000, DEV), A.Blocks8.empty(72, 20000, DEV)
+    x, y = torch.randint(-4, 5, (64, 20000)).float().to(DEV), torch.randint(-4, 5, (72, 20000)).float().to(DEV)
+    for m, q in ((x, a), (y, b)):
+        A.adloco_pack_blocks(ctx, m, q)
+    h, dy = torch.full((500, 64), 2.0, device=DEV), torch.randint(-3, 4, (500, 64)).float().to(DEV)      # h / sqrt(mean(h^2)) = 1
+    for limit in (1, 0):
+        ctx.set_tuning("scratch_limit_kb", limit)
+        out, sums = torch.full((64, 72), 7.0, device=DEV), torch.full((1, 64), 7.0, device=DEV)
+        A.adloco_block_product(ctx, a, b, out)
+        A.adloco_rms_norm_backward(ctx, h, None, dy, 1e-30, gain_sums=sums)
+        np.testing.assert_array_equal(host(out), host(x) @ host(y).T)
+        np.testing.assert_allclose(host(sums)[0], host(dy).sum(0), rtol=0, atol=600 * U * 1500)
+    ctx.close()
+
+
 def test_captured_without_scratch_is_right():
     """A context whose first split sum is captured has no scratch for it: it takes the sums whole."""
     ctx = A.Context(0)
