@@ -608,8 +608,7 @@ def _on(ctx: Context, t, name: str):
 
 
 def _layer_stream(ctx: Context, stream) -> int:
-    import torch
-    return torch._C._cuda_getCurrentRawStream(ctx.device) if stream is None else stream.cuda_stream
+    return _raw_stream(ctx.device) if stream is None else stream.cuda_stream
 
 
 def _blocks8(ctx: Context, b: Optional[Blocks8], name: str):
@@ -617,26 +616,27 @@ def _blocks8(ctx: Context, b: Optional[Blocks8], name: str):
     if b is None:
         return None
     data, exponent, rows, cols = b.data, b.exponent, b.rows, b.cols
-    wide = (cols + 127) // 128 * 128
-    _on(ctx, data, name)
-    _on(ctx, exponent, name)
-    if not (_is_bytes(data, rows, wide) and _is_bytes(exponent, wide // 128, rows)):
-        raise ValueError(f"{name}: data must be uint8 [>= {rows}, >= {wide}] and exponent uint8 [>= {wide // 128}, >= {rows}], "
+    blocks = (cols + 127) // 128
+    if data.get_device() != ctx.device or exponent.get_device() != ctx.device:
+        _on(ctx, data, name)
+        _on(ctx, exponent, name)
+    row, plane = _row_bytes(data, rows, blocks * 128), _row_bytes(exponent, blocks, rows)
+    if row < 0 or plane < 0:
+        raise ValueError(f"{name}: data must be uint8 [>= {rows}, >= {blocks * 128}] and exponent uint8 [>= {blocks}, >= {rows}], "
                          f"both with unit stride along their rows; got {tuple(data.shape)} {data.dtype} and "
                          f"{tuple(exponent.shape)} {exponent.dtype}")
-    return Blocks8Desc(data.data_ptr(), exponent.data_ptr(), rows, cols, _row_bytes(data), _row_bytes(exponent))
+    return Blocks8Desc(data.data_ptr(), exponent.data_ptr(), rows, cols, row, plane)
 
 
-def _is_bytes(t, rows: int, width: int) -> bool:
-    import torch
-    if t.dtype is not torch.uint8 or t.dim() != 2:
-        return False
-    r, w = t.shape
-    return r >= rows and w >= width and (w <= 1 or t.stride(1) == 1)
-
-
-def _row_bytes(t) -> int:
-    return t.stride(0) if t.size(0) > 1 else t.size(1)
+def _row_bytes(t, rows: int, width: int) -> int:
+    """Row stride of a byte matrix of at least rows x width, -1 if it is not one."""
+    shape = t.shape
+    if t.dtype is not _uint8 or len(shape) != 2 or shape[0] < rows or shape[1] < width:
+        return -1
+    stride, unit = t.stride()
+    if unit != 1 and shape[1] > 1:
+        return -1
+    return stride if shape[0] > 1 else shape[1]
 
 
 def _matrix(ctx: Context, t, name: str, shape=None, dtype=None):
@@ -644,8 +644,9 @@ def _matrix(ctx: Context, t, name: str, shape=None, dtype=None):
     None.  shape, dtype: what it has to be."""
     if t is None:
         return None, 0
-    _on(ctx, t, name)
-    if t.dim() < 1 or (shape is not None and (t.shape != shape or t.dtype is not dtype)):
+    if t.get_device() != ctx.device:
+        _on(ctx, t, name)
+    if t.dim() < 1 if shape is None else t.dtype is not dtype or t.shape != shape:
         raise ValueError(f"{name} must be {'a matrix' if shape is None else f'{tuple(shape)} {dtype}'}, got "
                          f"{tuple(t.shape)} {t.dtype}")
     if t.is_contiguous():
@@ -670,13 +671,18 @@ def _matrix(ctx: Context, t, name: str, shape=None, dtype=None):
 
 
 _LAYER_DTYPES = {}
+_uint8 = _float32 = _raw_stream = None
 
 
 def _layer_dtype(dtype, name: str) -> int:
-    import torch
-    if not _LAYER_DTYPES:
-        _LAYER_DTYPES.update({torch.float32: ADLOCO_F32, torch.bfloat16: ADLOCO_BF16, torch.float16: ADLOCO_F16})
+    """Code of an element type; the first thing that a layer operator asks for."""
     code = _LAYER_DTYPES.get(dtype)
+    if code is None:
+        global _uint8, _float32, _raw_stream
+        import torch
+        _uint8, _float32, _raw_stream = torch.uint8, torch.float32, torch._C._cuda_getCurrentRawStream
+        _LAYER_DTYPES.update({torch.float32: ADLOCO_F32, torch.bfloat16: ADLOCO_BF16, torch.float16: ADLOCO_F16})
+        code = _LAYER_DTYPES.get(dtype)
     if code is None:
         raise TypeError(f"{name} has dtype {dtype}, expected float32, bfloat16 or float16")
     return code
@@ -691,11 +697,11 @@ def _mask(p: float, seed: int, first_row: int):
 
 
 def _gain(ctx: Context, gain, d: int):
-    import torch
     if gain is None:
         return None
-    _on(ctx, gain, "gain")
-    if gain.dtype is not torch.float32 or gain.numel() != d or not gain.is_contiguous():
+    if gain.get_device() != ctx.device:
+        _on(ctx, gain, "gain")
+    if gain.dtype is not _float32 or gain.numel() != d or not gain.is_contiguous():
         raise ValueError(f"gain must be a contiguous fp32 tensor of {d} values")
     return gain.data_ptr()
 
@@ -756,7 +762,6 @@ def adloco_rms_norm_backward(ctx: Context, h, gain, dy, eps: float, dh_out=None,
                              p: float = 0.0, seed: int = 0, first_row: int = 0, stream=None):
     """Gradient of the norm: dh_out = dh_in + d y / d h^T dy, dx_out = dropout(dh_out), gain_sums fp32 [B, d] = the gain's
     gradient of every sample, whose rows are h's in order (B divides their number; None: one sample)."""
-    import torch
     shape, dtype = h.shape, h.dtype
     code = _layer_dtype(dtype, "h")
     ph, sh = _matrix(ctx, h, "h")
@@ -769,7 +774,7 @@ def adloco_rms_norm_backward(ctx: Context, h, gain, dy, eps: float, dh_out=None,
     if gain_sums is not None:
         _on(ctx, gain_sums, "gain_sums")
         B = gain_sums.shape[0] if gain_sums.dim() == 2 else -1
-        if gain_sums.dtype is not torch.float32 or B < 0 or gain_sums.shape[1] != d or not gain_sums.is_contiguous() or (B == 0 and rows) or (B and rows % B):
+        if gain_sums.dtype is not _float32 or B < 0 or gain_sums.shape[1] != d or not gain_sums.is_contiguous() or (B == 0 and rows) or (B and rows % B):
             raise ValueError(f"gain_sums must be a contiguous fp32 tensor [B, {d}] with B dividing {rows} rows")
         sums = gain_sums.data_ptr()
     io = NormBackwardIo(ph, py, pi, _gain(ctx, gain, d), po, px, sums, sh, sy, si, so, sx)
