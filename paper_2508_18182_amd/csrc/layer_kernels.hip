@@ -398,8 +398,11 @@ constexpr int norm_waves(int wide) { return wide <= 512 ? 1 : wide <= 1024 ? 2 :
 
 template <typename E, bool FAST> struct LaunchNorm {
   static hipError_t run(const NormArgs& a, hipStream_t st) {
-    const long long most = (long long)kNumCu * 16 / norm_waves(a.wide);      // sixteen waves per compute unit
-    const dim3 grid(unsigned(a.rows < most ? a.rows : most));
+    // Sixteen waves per compute unit, which all run at once; where that leaves a workgroup eight rows or more, four each, dealt out
+    // as others end (at once / dealt out: 32768 x 2048 110 / 103 us, 32768 x 768 with dropout 51 / 46, one row each 107 / 49; at
+    // five rows, 2500 x 5000, at once 26, dealt out 27).
+    const long long most = (long long)kNumCu * 16 / norm_waves(a.wide);
+    const dim3 grid(unsigned(a.rows < most ? a.rows : a.rows < 8 * most ? most : (a.rows + 3) / 4));
 #define ADLOCO_CALL(NV, WAVES) hipLaunchKernelGGL((rms_norm_kernel<E, NV, WAVES, FAST>), grid, dim3(64 * WAVES), 0, st, a)
     ADLOCO_NORM_SHAPE(a.wide, ADLOCO_CALL);
 #undef ADLOCO_CALL

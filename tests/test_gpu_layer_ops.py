@@ -384,7 +384,15 @@ def check_y8(y8, want, off):
 
 @pytest.mark.parametrize("rows", [1, 2, 31, 4096, 5001])
 def test_rms_norm_row_counts(ctx, rows):
-    d = 264
+    row_count(ctx, rows, 264)
+
+
+@pytest.mark.parametrize("rows,d", [(33001, 40), (4105, 2056)])
+def test_rms_norm_of_many_rows_a_workgroup(ctx, rows, d):
+    row_count(ctx, rows, d)
+
+
+def row_count(ctx, rows, d):
     x, res, gain = norm_inputs(rows, d, torch.bfloat16)
     want = lo.rms_norm(host(x) + host(res), host(gain), 1e-6)
     h = host(x) + host(res)
