@@ -61,7 +61,7 @@ template <typename E, bool FAST> __global__ __launch_bounds__(kPackThreads) void
     }
 #pragma unroll
     for (int i = 0; i < R; ++i) {
-      widen_eight<E>(raw[i], v[i]);
+      widen_eight<E, FAST>(raw[i], cg * 8, left, v[i]);
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[i][j] = r0 + i < a.rows && cg * 8 + j < left ? v[i][j] : 0.f;
     }

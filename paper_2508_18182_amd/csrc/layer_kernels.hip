@@ -43,8 +43,8 @@ template <typename E, bool FAST> __global__ __launch_bounds__(64) void dropout_k
 // h = residual + dropout(x);  y = h * rsqrt(mean(h^2) + eps) * gain, in the type of x and / or in 8-bit blocks.
 // A row belongs to WAVES waves, a lane holds NV groups of eight columns of it in registers.  The statistics are of h in
 // fp32, before it is rounded for the store.  Where the squares of a row leave fp32 (|h| > 1.8e19), they are formed again of
-// 2^-96 h: a row of large finite values keeps its norm.  32768 x 2048 bf16 with residual, h, y and y8: 100 us, 6.0 TB/s;
-// 5005 x 771 fp32, whose rows share no alignment: 14 us, 4.4 TB/s; one row: 3 us, four dependent trips to memory and back.
+// 2^-96 h: a row of large finite values keeps its norm.  32768 x 2048 bf16 with residual, h, y and y8: 98 us, 6.2 TB/s;
+// 5005 x 771 fp32, whose rows share no alignment: 13 us, 4.7 TB/s; one row: 3 us, four dependent trips to memory and back.
 // ---------------------------------------------------------------------------------------------------------------------
 struct NormArgs {
   const void* x;
@@ -232,9 +232,9 @@ __global__ __launch_bounds__(64 * WAVES) void rms_norm_backward_kernel(NormBackA
     float h[NV][8], y[NV][8], in[NV][8];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      widen_eight<E>(rh[i], h[i]);
-      widen_eight<E>(ry[i], y[i]);
-      if (a.dh_in) widen_eight<E>(ri[i], in[i]);
+      widen_eight<E, FAST>(rh[i], c0 + i * 512 * WAVES, a.d, h[i]);
+      widen_eight<E, FAST>(ry[i], c0 + i * 512 * WAVES, a.d, y[i]);
+      if (a.dh_in) widen_eight<E, FAST>(ri[i], c0 + i * 512 * WAVES, a.d, in[i]);
     }
     if (ahead && row + 1 < last) fetch(row + 1);
     float s[2] = {0.f, 0.f}, eps = a.eps, pre = 1.f;

@@ -120,6 +120,18 @@ def test_dropout_of_strided_rows_leaves_the_rest(ctx, pad, offset):
 
 # ---- 8-bit blocks ---------------------------------------------------------------------------
 
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("d", [*range(1, 33), 511, 513, 515, 518])
+def test_every_length_of_a_row_behind_its_groups_of_eight(ctx, d, dtype):
+    dt, rows = TYPES[dtype], 9
+    x, res = rand(d, (rows, d), dt), rand(d + 1, (rows, d), dt)
+    out, buf = apart(torch.zeros_like(x), 3, 1)
+    A.adloco_dropout(ctx, apart(x, 5, 2)[0], out, 0.0, 1, residual=apart(res, 1)[0])
+    assert torch.equal(out, (x.float() + res.float()).to(dt))          # nothing dropped: one fp32 sum, rounded once
+    out.fill_(7.0)
+    assert bool((buf == 7).all())
+
+
 def codes_of(b):
     """(values, exponents) of a Blocks8 on the host, the padding among them."""
     wide = -(-b.cols // 128) * 128
