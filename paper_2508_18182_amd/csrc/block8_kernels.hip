@@ -483,7 +483,7 @@ __global__ __launch_bounds__(256, (TileShape<MB, NB, EXACT>::resident)) void pro
 #pragma unroll
     for (int i = 0; i < T::second_loads; ++i) load_second(buf, i);
   };
-  // Element j of block (m, n): row (kg * 4 + j) * MB + m of the wave tile, column l16 * NB + n.  Three ways out, each short
+  // Element j of block (m, n): row (kg * 4 + j) * MB + m of the wave tile, column l16 * NB + n.  Four ways out, each short
   // enough for the instruction cache (checks woven into one of them: 60 KB of code, 4 us a tile).
   auto rows_out = [&](int first, int count, auto put) {
 #pragma unroll
@@ -508,9 +508,18 @@ __global__ __launch_bounds__(256, (TileShape<MB, NB, EXACT>::resident)) void pro
       E* const out = static_cast<E*>(p.out) + (m0 + row0) * p.os + n0 + wn + l16 * NB;
       rows_out(0, MB, [&](int m, int j, const float (&v)[NB]) { store_row<E, NB>(out + (j * MB + m) * p.os, v, p.accumulate != 0); });
       return !p.accumulate;
+    } else if (p.vec && p.N % NB == 0) {
+      // a tile on the edge: a lane's columns are all there or all not
+      const int below = p.M - m0 - row0;
+      E* const out = static_cast<E*>(p.out) + (m0 + row0) * p.os + n0 + wn + l16 * NB;
+      if (n0 + wn + l16 * NB < p.N)
+        rows_out(0, MB, [&](int m, int j, const float (&v)[NB]) {
+          if (j * MB + m < below) store_row<E, NB>(out + (j * MB + m) * p.os, v, p.accumulate != 0);
+        });
     } else {
-      // a tile on the edge, or rows that are not aligned: 64 rows of the wave tile at a time through LDS, value by value
-      constexpr int passes = MB / 4;
+      // rows that are not aligned, or no whole number of a lane's columns: 64 rows of the wave tile at a time through LDS, value
+      // by value, eight under way
+      constexpr int passes = MB / 4, wide = T::wave_n / 64, ahead_rows = 8 / wide;
       product_wait<0>();
       meet();
       float* const mine = reinterpret_cast<float*>(lds) + wave * (64 * T::wave_n);
@@ -525,17 +534,23 @@ __global__ __launch_bounds__(256, (TileShape<MB, NB, EXACT>::resident)) void pro
         const int below = p.M - m0 - wm, right = p.N - n0 - wn;
         E* const out = static_cast<E*>(p.out) + (m0 + wm) * p.os + n0 + wn;
 #pragma unroll 1
-        for (int i = 0; i < 64; ++i) {
-          const int r = (i >> 2) * MB + h * 4 + (i & 3);
-          if (r >= below) continue;
+        for (int i0 = 0; i0 < 64; i0 += ahead_rows) {
+          float v[ahead_rows][wide];
 #pragma unroll
-          for (int c = 0; c < T::wave_n; c += 64)
-            if (c + lane < right) {
-              E* q = out + r * p.os + c + lane;
-              const float v = mine[i * T::wave_n + c + lane];
-              if constexpr (std::is_same<E, float>::value) *q = p.accumulate ? *q + v : v;
-              else *q = E(v);
-            }
+          for (int i = 0; i < ahead_rows; ++i)
+#pragma unroll
+            for (int c = 0; c < wide; ++c) v[i][c] = mine[(i0 + i) * T::wave_n + c * 64 + lane];
+#pragma unroll
+          for (int i = 0; i < ahead_rows; ++i) {
+            const int r = ((i0 + i) >> 2) * MB + h * 4 + ((i0 + i) & 3);
+#pragma unroll
+            for (int c = 0; c < wide; ++c)
+              if (r < below && c * 64 + lane < right) {
+                E* q = out + r * p.os + c * 64 + lane;
+                if constexpr (std::is_same<E, float>::value) *q = p.accumulate ? *q + v[i][c] : v[i][c];
+                else *q = E(v[i][c]);
+              }
+          }
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       }
