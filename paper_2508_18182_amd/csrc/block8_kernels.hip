@@ -771,7 +771,7 @@ template <typename E> hipError_t launch_product(const ProductArgs& p, bool large
 // and 6.5 to start and store one; 1.7 and the partial tiles' way out and back for a second kernel.  The choice is within 4 %
 // of the best one on average.  Measured, few rows / small tiles / small tiles in 4 pieces / large: 3 x 5632 x 2048 7 / 11 / 11
 // / 23, 64 x 8192 x 8192 - / 29 / 20 / 60, 512 x 5632 x 2048 - / 15 / 26 / 35, 32768 x 5632 x 2048 - / 376 / - / 300 us.
-// Rows of the output that are not 16-byte aligned cost a large tile 12 us more, a small one 1 (32001 x 2044 x 1024: 82 / 124).
+// Rows of the output that are not 16-byte aligned count 12 us more for a large tile (32001 x 2044 x 1024: small 78, large 104).
 struct ProductChoice { int kernel, pieces; };          // kernel: 1 few rows, 4 small tiles, 8 large ones
 ProductChoice choose_product(long long M, long long N, int steps, bool fp32, bool aligned, int kernel, int pieces, bool split) {
   ProductChoice best{4, 1};
