@@ -17,6 +17,7 @@ ADLOCO_ACCUMULATE = 0x1
 ADLOCO_SUM_ONLY = 0x2
 ADLOCO_GRAD_PROVIDED = 0x1
 ADLOCO_KIND_LINEAR, ADLOCO_KIND_VECTOR, ADLOCO_KIND_EMBED, ADLOCO_KIND_SAMPLE_SUMS = 0x00, 0x10, 0x20, 0x40
+ADLOCO_KIND_MASK = 0xF0
 ADLOCO_BROADCAST = 0x1
 ADLOCO_BIASED_VAR = 0x1
 ADLOCO_ALLOW_SHRINK = 0x2
@@ -289,6 +290,20 @@ def _dev_ptr(t, dtype=None, numel=None, name="tensor") -> C.c_void_p:
     return C.c_void_p(t.data_ptr())
 
 
+def _sample_stride(t, where: str, B: int, d: Optional[int] = None) -> int:
+    """Row stride of per-sample sums, fp32 [B, d] on the GPU."""
+    import torch
+    if (not t.is_cuda or t.dtype != torch.float32 or t.dim() != 2 or t.shape[0] != B or (d is not None and t.shape[1] != d)
+            or (t.stride(1) != 1 and t.shape[1] > 1)):
+        raise ValueError(f"{where}: sums must be a GPU fp32 tensor [B={B},d{'' if d is None else f'={d}'}] with unit stride in d, "
+                         f"got {tuple(t.shape)} {t.dtype}")
+    if B == 1:
+        return t.shape[1]
+    if t.stride(0) < t.shape[1]:                  # (0, of an expanded tensor, would stand for d_out)
+        raise ValueError(f"{where}: rows of sums must not share memory")
+    return t.stride(0)
+
+
 def make_layer_descs(layers: Sequence[dict], B: int, T: int, dtype: int):
     """layers: dicts with a [B,T,d_in], delta [B,T,d_out], optional grad_sum [d_out,d_in] fp32,
     optional provided=True.  Token rows may be strided views (last dim contiguous).
@@ -314,15 +329,12 @@ def make_layer_descs(layers: Sequence[dict], B: int, T: int, dtype: int):
         flags = ADLOCO_GRAD_PROVIDED if l.get("provided") else 0
         if kind == "sample_sums":
             d = l["sums"]
-            if not d.is_cuda or d.dtype != torch.float32 or d.dim() != 2 or d.shape[0] != B or d.stride(1) != 1:
-                raise ValueError(f"layer {i}: sums must be a GPU fp32 tensor [B={B},d] with unit stride in d, got "
-                                 f"{tuple(d.shape)} {d.dtype}")
-            if B > 1 and d.stride(0) < d.shape[1]:        # (0, of an expanded tensor, would stand for d_out)
-                raise ValueError(f"layer {i}: rows of sums must not share memory")
+            d_stride = _sample_stride(d, f"layer {i}", B)
             d = d.unsqueeze(1)
         else:
             d = l["delta"]
             check_rows(i, "delta", d)
+            d_stride = d.stride(1)
         if kind == "sample_sums":
             a_ptr, a_stride, d_in, gshape = None, 0, 1, (d.shape[2],)
             flags |= ADLOCO_KIND_SAMPLE_SUMS
@@ -357,7 +369,7 @@ def make_layer_descs(layers: Sequence[dict], B: int, T: int, dtype: int):
         arr[i].d_in = d_in
         arr[i].d_out = d.shape[2]
         arr[i].a_row_stride = a_stride
-        arr[i].delta_row_stride = d.stride(0) if kind == "sample_sums" and B > 1 else d.stride(1) if kind != "sample_sums" else 0
+        arr[i].delta_row_stride = d_stride
         arr[i].grad_sum = g.data_ptr() if g is not None else None
         arr[i].flags = flags
         arr[i].reserved = 0
@@ -802,7 +814,8 @@ def adloco_round(ctx: Context, cfg: dict, trainers: Sequence[dict], blocks: Sequ
     reordered / shortened like the C array when trainers merge.
     blocks: template of the parameter blocks: dicts {d_in, d_out, kind ("linear" | "vector" | "sample_sums")}.
     batch_fn(uid, worker, inner_step, micro_step, b, theta_ptr) -> list of dicts {a | x, delta}
-    (GPU tensors [b, T, .]; for sample_sums {sums}, fp32 [b, d]) in block order; the tensors are kept alive until the round returns.
+    (GPU tensors [b, T, .]; for sample_sums {sums}, fp32 [b, d_out], samples may be a stride apart) in block order; the
+    tensors are kept alive until the round returns.
     Returns the reports of the remaining trainers."""
     import torch
     lib = load_library()
@@ -849,9 +862,16 @@ def adloco_round(ctx: Context, cfg: dict, trainers: Sequence[dict], blocks: Sequ
             for l in range(n):
                 e = got[l]
                 desc = layers[l]        # (every index makes a ctypes object of its own)
-                if "sums" in e:
-                    desc.delta = _dev_ptr(e["sums"], torch.float32, int(b) * desc.d_out, "sums").value
+                # what is read of an entry goes by the block's kind: the kernels trust it for how many rows there are
+                sums = e.get("sums")
+                if desc.flags & ADLOCO_KIND_MASK == ADLOCO_KIND_SAMPLE_SUMS:
+                    if sums is None:
+                        raise ValueError(f"block {l}: a block of per-sample sums needs sums, got {sorted(e)}")
+                    desc.delta_row_stride = _sample_stride(sums, f"block {l}", int(b), desc.d_out)
+                    desc.delta = sums.data_ptr()
                     continue
+                if sums is not None:
+                    raise ValueError(f"block {l}: sums are for blocks of per-sample sums only")
                 d = e["delta"]
                 desc.delta = d.data_ptr()
                 desc.delta_row_stride = d.stride(1)
