@@ -62,7 +62,7 @@ template <typename E, bool FAST> __device__ __forceinline__ void store_eight(E* 
   for (int j = 0; j < 8; ++j) r[j] = E(v[j]);
   if constexpr (FAST) {
     if (c < d) __builtin_nontemporal_store(r, reinterpret_cast<eight<E>*>(row + c));
-  } else if (c + 8 <= d) {
+  } else if (c <= d - 8) {                             // (d may be 2^31 - 1: c + 8 would overflow)
     __builtin_memcpy(row + c, &r, sizeof r);
   } else if (c < d) {                                  // four, two and one of them
     const int n = d - c;
