@@ -158,11 +158,13 @@ __device__ __forceinline__ void mark_eight(const float (&v)[8], uint2& o) {
 }
 // y, the fp32 rounding of y + rest, with its last bit set where something was rounded away (towards what it was): rounded
 // once more to fewer bits, it gives what y + rest gives.  Without it, one value in 2^20 comes to lie just between two e4m3
-// values by its first rounding, and goes a whole step the wrong way half the time.
+// values by its first rounding, and goes a whole step the wrong way half the time.  An infinite or NaN y (whose
+// rest is not finite either) stays what it is.
 __device__ __forceinline__ float round_to_odd(float y, float rest) {
   const unsigned u = __float_as_uint(y);
   const int towards = int((__float_as_uint(rest) ^ u)) >> 31 | 1;        // away from zero: 1, towards it: -1
-  const bool cut = (rest < 0.f || rest > 0.f) && (u & 1u) == 0u && (u & 0x7fffffffu) != 0u;
+  constexpr int finite = 0x198;                         // class of rest: normal or subnormal, of either sign, and not zero
+  const bool cut = __builtin_amdgcn_classf(rest, finite) && (u & 1u) == 0u && (u & 0x7fffffffu) != 0u;
   return __uint_as_float(cut ? u + unsigned(towards) : u);
 }
 // Maximum over groups of 16 lanes, in all of them.  All lanes of a group have to be there.

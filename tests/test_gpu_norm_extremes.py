@@ -1,0 +1,110 @@
+"""The RMS norm and its backward pass at the ends of fp32: outputs that overflow, values next to the middle of two 8-bit or
+16-bit ones, gradients and rows whose products leave the range that their quotients stay in."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2508_18182_amd as A
+from oracle import layer_oracle as lo
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+U = 2.0**-24
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = A.Context(0)
+    yield c
+    c.close()
+
+
+def host(t):
+    return t.detach().cpu().double().numpy()
+
+
+def codes_of(b):
+    wide = -(-b.cols // 128) * 128
+    return lo.e4m3_table()[b.data[:, :wide].cpu().numpy()], b.exponent[:, :b.rows].cpu().numpy()
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("d", [128, 300, 2048])
+def test_outputs_beyond_fp32(ctx, d, dtype):
+    """y where it overflows is infinite and NaN in 8 bits, as packing it in fp32 gives; the rest of its block keeps its own
+    exponent.  Rows of 16 values +- 9, 5, 3, 3, 1, 1, 1, 1 (mean square 16, twice) and zeros: n is what h is, over a power of
+    two or the square root of one."""
+    eight = torch.tensor([9.0, -5, 3, 3, 1, -1, 1, 1])
+    h = torch.zeros(3, d)
+    h[:, :16] = eight.repeat(2)
+    h[1] = -h[1]
+    h[2, 0] = 0.0                                      # (0 times a large gain)
+    x = h.to(TYPES[dtype]).to(DEV)
+    gain = torch.full((d,), 0.5)
+    gain[0], gain[1], gain[9] = 3.0e38, -3.0e38, 3.4e38
+    y, y32, y8, again = torch.empty_like(x), torch.empty(3, d, device=DEV), A.Blocks8.empty(3, d, DEV), A.Blocks8.empty(3, d, DEV)
+    A.adloco_rms_norm(ctx, x, gain.to(DEV), 1e-30, y=y, y8=y8)
+    A.adloco_rms_norm(ctx, x.float(), gain.to(DEV), 1e-30, y=y32)
+    want = lo.rms_norm(h.double().numpy(), gain.double().numpy(), 1e-30)
+    over = np.abs(want) > 3.4028235e38                 # (the nearest of them are a factor of 1.2 away)
+    assert over.sum() >= 5
+    got = host(y32)
+    assert np.array_equal(np.isinf(got), over) and np.array_equal(np.sign(got[over]), np.sign(want[over]))
+    assert np.array_equal(np.isinf(host(y))[over], np.ones(over.sum(), bool)) and not np.isnan(host(y)).any()
+    codes, exps = codes_of(y8)
+    A.adloco_pack_blocks(ctx, y32, again)
+    assert np.array_equal(np.isnan(codes[:, :d]), over)
+    assert np.array_equal(np.isnan(codes_of(again)[0][:, :d]), over) and np.array_equal(exps, codes_of(again)[1])
+    finite = np.where(over, 0.0, want)
+    power = np.repeat(np.exp2(exps.astype(np.float64) - 127).T, 128, axis=1)[:, :d]
+    assert np.array_equal(exps, lo.pack(finite)[1])
+    off = np.abs(codes[:, :d] * power - finite)
+    assert (off[~over] <= ((2.0**-4 * (1 + 64 * U) + 64 * U) * np.abs(finite) + 2.0**-10 * power)[~over]).all()
+
+
+def next_to_middles(bits):
+    """Gains such that a value 5/4 (or 3/4, 9/4) times one lies within 2^-24 of the middle of two neighbouring numbers of `bits`
+    mantissa bits, on either side of it and never on it: rounded to fp32 first, it often is that middle."""
+    out = []
+    for over in (9, 5, 3):
+        for i in range(2**bits) if bits < 4 else range(0, 2**bits, 5):
+            middle = 1 + (2 * i + 1) * 2.0**-(bits + 1)
+            g = np.float32(middle * 4 / over)
+            out += [(over, v) for v in (g, np.nextafter(g, np.float32(0)), np.nextafter(g, np.float32(9)))
+                    if float(v) * over / 4 != middle]
+    return out
+
+
+@pytest.mark.parametrize("out,dtype", [("y8", "f32"), ("y8", "bf16"), ("y", "bf16"), ("y", "f16")])
+def test_values_next_to_the_middle_of_two_are_rounded_once(ctx, out, dtype):
+    """Rows of +- 9, 5, 3, 3, 1, 1, 1, 1: their mean square is 16 (eps 2^-126 is lost beside it even in fp64), n = h / 4 is exact,
+    and n times a gain of 24 bits is exact in fp64, so that the oracle's rounding of it is the rounding of the value itself."""
+    bits = {"y8": 3, "bf16": 7, "f16": 10}[out if out == "y8" else dtype]
+    cases = next_to_middles(bits)
+    d = 1 << (8 * len(cases) - 1).bit_length()
+    h, gain = np.tile([9.0, -5, 3, 3, 1, -1, 1, 1], d // 8), np.ones(d, np.float32)
+    at = {9: 0, 5: 1, 3: 2}
+    for k, (over, g) in enumerate(cases):
+        gain[8 * k + at[over]] = g
+    x = torch.from_numpy(np.stack([h, -h])).to(TYPES[dtype]).to(DEV)
+    want = np.stack([h, -h]) / 4 * gain.astype(np.float64)
+    twice = np.float32(want).astype(np.float64)        # what a first rounding to fp32 makes of them
+    if out == "y8":
+        y8 = A.Blocks8.empty(2, d, DEV)
+        A.adloco_rms_norm(ctx, x, torch.from_numpy(gain).to(DEV), 2.0**-126, y8=y8)
+        codes, exps = codes_of(y8)
+        right, other = lo.pack(want), lo.pack(twice)
+        np.testing.assert_array_equal(exps, right[1])
+        np.testing.assert_array_equal(codes, right[0])
+        assert (right[0] != other[0]).sum() >= 8       # (the inputs tell one from the other)
+    else:
+        y = torch.empty_like(x)
+        A.adloco_rms_norm(ctx, x, torch.from_numpy(gain).to(DEV), 2.0**-126, y=y)
+
+        def rounded(v):
+            step = np.exp2(np.floor(np.log2(np.abs(v))) - bits)
+            return np.rint(v / step) * step
+        np.testing.assert_array_equal(host(y), rounded(want))
+        assert (rounded(want) != rounded(twice)).sum() >= 8
