@@ -62,6 +62,7 @@ struct NormArgs {
   DropoutArgs m;
 };
 
+constexpr float kLargest = 3.402823466e38f;       // the largest fp32 number
 constexpr float kTiny = 1.262177448353619e-29f;   // 2^-96: 16384 squares of the largest fp32 number fit
 
 // Sums over the row of a few values at once; `slot` alternates from row to row, so that one barrier is enough.
@@ -149,7 +150,9 @@ template <typename E, int NV, int WAVES, bool FAST> __global__ __launch_bounds__
       float odd[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const float n = h[i][j] * r_hi, rest = fmaf(h[i][j], r_lo, fmaf(h[i][j], r_hi, -n)) * g[i][j];
+        // (clamped: an infinite gain would make it infinite, of either sign, or NaN)
+        const float n = h[i][j] * r_hi, error = fmaf(h[i][j], r_lo, fmaf(h[i][j], r_hi, -n));
+        const float rest = __builtin_amdgcn_fmed3f(error * g[i][j], -kLargest, kLargest);
         h[i][j] = fmaf(n, g[i][j], rest);
         odd[j] = round_to_odd(h[i][j], fmaf(n, g[i][j], -h[i][j]) + rest);
       }

@@ -64,6 +64,23 @@ def test_outputs_beyond_fp32(ctx, d, dtype):
     assert (off[~over] <= ((2.0**-4 * (1 + 64 * U) + 64 * U) * np.abs(finite) + 2.0**-10 * power)[~over]).all()
 
 
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_gains_that_are_not_finite(ctx, dtype):
+    x = torch.tensor([[9.0, -5, 3, 3, 1, -1, 1, 0] * 3], dtype=TYPES[dtype], device=DEV)
+    x = x * torch.tensor([1.0, 0.37], device=DEV)[:, None].to(x.dtype)
+    gain = torch.full((24,), 0.3, device=DEV)
+    gain[0:3], gain[5], gain[7], gain[15], gain[16] = float("inf"), float("-inf"), float("inf"), 0.0, float("nan")
+    y, y8 = torch.empty_like(x), A.Blocks8.empty(2, 24, DEV)
+    A.adloco_rms_norm(ctx, x, gain, 1e-5, y=y, y8=y8)
+    with np.errstate(invalid="ignore"):
+        want = lo.rms_norm(host(x), host(gain), 1e-5)
+    got = host(y)
+    wild = ~np.isfinite(want)
+    assert np.array_equal(got[wild], want[wild], equal_nan=True) and np.isfinite(got[~wild]).all()
+    np.testing.assert_allclose(got[~wild], want[~wild], rtol=torch.finfo(y.dtype).eps / 2 * (1 + 64 * U) + 64 * U)
+    assert np.array_equal(np.isnan(codes_of(y8)[0][:, :24]), wild)
+
+
 def next_to_middles(bits):
     """Gains such that a value 5/4 (or 3/4, 9/4) times one lies within 2^-24 of the middle of two neighbouring numbers of `bits`
     mantissa bits, on either side of it and never on it: rounded to fp32 first, it often is that middle."""
