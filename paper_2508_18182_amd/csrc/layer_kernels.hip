@@ -252,7 +252,7 @@ __global__ __launch_bounds__(64 * WAVES) void rms_norm_backward_kernel(NormBackA
     if (!(s[0] <= 3.402823466e38f)) {               // (the same for the whole row)
       s[0] = s[1] = 0.f;
       pre = kTiny;
-      eps *= kTiny * kTiny;
+      eps = float(double(eps) * (double(kTiny) * kTiny));   // (the product of the two is 0 in fp32)
 #pragma unroll
       for (int i = 0; i < NV; ++i)
 #pragma unroll

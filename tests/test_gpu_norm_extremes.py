@@ -125,3 +125,40 @@ def test_values_next_to_the_middle_of_two_are_rounded_once(ctx, out, dtype):
             return np.rint(v / step) * step
         np.testing.assert_array_equal(host(y), rounded(want))
         assert (rounded(want) != rounded(twice)).sum() >= 8
+
+
+# ---- backward -------------------------------------------------------------------------------
+# u = 2^-24.  A sum over a row is 64 terms in a row and 8 in a tree, all its terms are off by three roundings: with n and r off by
+# six each, w - n mean(w n) is off by 90 u (|w| + |n| mean|w n|) at most (the bound of ordinary rows, 80 u, and the scales').
+
+BACK_TOL = 90 * U
+
+
+def backward(ctx, h, gain, dy, eps, dtype=torch.float32):
+    h, dy = (torch.from_numpy(np.asarray(v, np.float32)).to(dtype).to(DEV) for v in (h, dy))
+    g = None if gain is None else torch.from_numpy(np.asarray(gain, np.float32)).to(DEV)
+    dh, sums = torch.empty_like(h), torch.empty(h.shape, device=DEV)
+    A.adloco_rms_norm_backward(ctx, h, g, dy, eps, dh, gain_sums=sums)
+    hh, yy, gg = host(h), host(dy), np.ones(h.shape[1]) if g is None else host(g)
+    grad, parts = lo.rms_norm_backward(hh, gg, yy, eps)
+    r = 1 / np.sqrt((hh * hh).mean(1, keepdims=True) + eps)
+    n, w = hh * r, gg * yy
+    assert np.abs(grad).max() < 1e38 and np.abs(parts).max() < 1e38    # (the gradients are finite)
+    half = torch.finfo(dtype).eps / 2
+    tol = BACK_TOL * r * (np.abs(w) + np.abs(n) * np.abs(w * n).mean(1, keepdims=True))
+    least = torch.finfo(dtype).smallest_normal * torch.finfo(dtype).eps
+    off = np.abs(host(dh) - grad)
+    assert (off <= tol + half * np.abs(grad) * (1 + 1e-4) + least).all(), (off / tol).max(1)
+    np.testing.assert_array_less(np.abs(host(sums) - parts), BACK_TOL * np.abs(parts) + 2.0**-148)
+    return host(dh)
+
+
+def normal(seed, *shape):
+    return np.random.default_rng(seed).normal(size=shape)
+
+
+@pytest.mark.parametrize("d", [8192, 16384])
+def test_eps_counts_beside_large_rows(ctx, d):
+    """eps 1e30 beside the smallest mean squares whose sum leaves fp32, 2.6e34 to 7.7e34: it moves the root by 100 to 300 u."""
+    h = np.sign(normal(9, 3, d)) * np.sqrt(4.3e38 / d) * np.array([[1.0], [1.1], [1.2]])
+    backward(ctx, h, None, normal(10, 3, d) * 1e10, 1e30)
