@@ -182,6 +182,7 @@ template <typename E, int NV, int WAVES, bool FAST> __global__ __launch_bounds__
 //   dh = dh_in + r (w - n mean(w n)),  dx = dropout(dh),  gain_sums[sample] = sum_t dy n.
 // Both sums of a row are formed in one pass, r again from h, which is here anyway.  A group of WAVES waves takes a run of one
 // sample's rows in order and keeps its columns of sum dy n in registers; runs are added up in order by a second kernel.
+// Rows whose sums leave fp32 make further passes over their registers.
 // 32768 x 1024 bf16 with dh_in and dropout, 32 samples: 66 us, 5.1 TB/s, and 4.5 us for the runs (8 MB written and read again);
 // two rows ahead instead of one: the same (70.7 and 70.9 us in all), at 2048 columns worse (99 and 104).
 // ---------------------------------------------------------------------------------------------------------------------
@@ -240,7 +241,7 @@ __global__ __launch_bounds__(64 * WAVES) void rms_norm_backward_kernel(NormBackA
       if (a.dh_in) widen_eight<E, FAST>(ri[i], c0 + i * 512 * WAVES, a.d, in[i]);
     }
     if (ahead && row + 1 < last) fetch(row + 1);
-    float s[2] = {0.f, 0.f}, eps = a.eps, pre = 1.f;
+    float s[2] = {0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
@@ -249,21 +250,32 @@ __global__ __launch_bounds__(64 * WAVES) void rms_norm_backward_kernel(NormBackA
         s[1] = fmaf(g[i][j] * y[i][j], h[i][j], s[1]);
       }
     row_sums<WAVES, 2>(s, lds, slot++ & 3);
-    if (!(s[0] <= 3.402823466e38f)) {               // (the same for the whole row)
+    float r = rsqrtf(fmaf(s[0], a.inv_d, a.eps)), mean = s[1] * r * a.inv_d, out = r;
+    // Sums that left fp32 (the same for the whole row).  w h may where w n does not: above it, or below it if r is large, when a
+    // sum of 0 may be one of lost products.
+    if (!(s[0] <= kLargest && fabsf(mean) <= kLargest && (r <= 1024.f || fabsf(s[1]) >= 0x1p-100f))) {
+      const float down = fabsf(s[1]) < 1.f ? 1.f : 0x1p-24f;         // w may be as large as fp32, and |n| adds up to d
+      if (!(s[0] <= kLargest)) {
+        s[0] = s[1] = 0.f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            h[i][j] *= kTiny;
+            s[0] = fmaf(h[i][j], h[i][j], s[0]);
+          }
+        row_sums<WAVES, 2>(s, lds, slot++ & 3);
+        r = rsqrtf(fmaf(s[0], a.inv_d, float(double(a.eps) * (double(kTiny) * kTiny))));
+        out = r * kTiny;
+      }
       s[0] = s[1] = 0.f;
-      pre = kTiny;
-      eps = float(double(eps) * (double(kTiny) * kTiny));   // (the product of the two is 0 in fp32)
 #pragma unroll
       for (int i = 0; i < NV; ++i)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          h[i][j] *= kTiny;
-          s[0] = fmaf(h[i][j], h[i][j], s[0]);
-          s[1] = fmaf(g[i][j] * y[i][j], h[i][j], s[1]);
-        }
+        for (int j = 0; j < 8; ++j) s[1] = fmaf(g[i][j] * y[i][j] * down, h[i][j] * r, s[1]);
       row_sums<WAVES, 2>(s, lds, slot++ & 3);
+      mean = s[1] * a.inv_d / down;
     }
-    const float r = rsqrtf(fmaf(s[0], a.inv_d, eps)), mean = s[1] * r * a.inv_d, out = r * pre;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = c0 + i * 512 * WAVES;

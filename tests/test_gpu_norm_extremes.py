@@ -157,6 +157,43 @@ def normal(seed, *shape):
     return np.random.default_rng(seed).normal(size=shape)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [96, 771, 3000, 16384])
+def test_backward_where_only_the_product_overflows(ctx, d, dtype):
+    """Sums of h^2 within fp32, of w h beyond it."""
+    h, dy = normal(1, 6, d), normal(2, 6, d)
+    for i, (a, b) in enumerate([(1e15, 1e24), (1e10, 1e29), (1e15, 1e29), (3.0, 5e36), (1e2, 1e35), (1.0, 1.0)]):
+        h[i] *= a
+        dy[i] *= b
+    h[5, ::3] = 0
+    dy[0] = np.abs(dy[0]) * np.sign(h[0])              # every term of one sign
+    backward(ctx, h, 1 + 0.1 * normal(3, d), dy, 1e-5, TYPES[dtype])
+
+
+@pytest.mark.parametrize("d", [96, 3000])
+def test_backward_of_large_rows_with_large_gradients(ctx, d):
+    """h^2 beyond fp32 as well, with small, ordinary and large gradients, and terms that cancel."""
+    h, dy = normal(4, 7, d), normal(5, 7, d)
+    for i, (a, b) in enumerate([(1e25, 1e20), (1e30, 1e36), (5e37, 1.0), (1e22, 1e-10), (3e19, 1e18), (1e37, 1e-3)]):
+        h[i] *= a
+        dy[i] *= b
+    dy[4, d // 2:] = -dy[4, :d // 2]
+    h[4, d // 2:] = h[4, :d // 2]
+    backward(ctx, h, None, dy, 1e-5)
+
+
+@pytest.mark.parametrize("d", [96, 3000])
+def test_backward_of_small_rows_with_a_small_eps(ctx, d):
+    """Products of w and h below fp32, of w and n within it."""
+    h, dy = normal(6, 6, d), normal(7, 6, d)
+    for i, (a, b) in enumerate([(1e-17, 1e-24), (1e-16, 1e-28), (1e-18, 1e-10), (1e-18, 1.0), (1e-17, 1e-20)]):
+        h[i] *= a
+        dy[i] *= b
+    h[4], dy[5] = 0, 0
+    got = backward(ctx, h, 1 + 0.1 * normal(8, d), dy, 2e-38)
+    assert not got[5].any()
+
+
 @pytest.mark.parametrize("d", [8192, 16384])
 def test_eps_counts_beside_large_rows(ctx, d):
     """eps 1e30 beside the smallest mean squares whose sum leaves fp32, 2.6e34 to 7.7e34: it moves the root by 100 to 300 u."""
