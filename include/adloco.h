@@ -554,7 +554,8 @@ int adloco_rms_norm(adloco_ctx* ctx, const adloco_norm_io* io, int64_t rows, int
  *   gain_sums[i] = sum over the T rows of sample i of dy n
  *   h, dy, dh, dx  [B * T, d]; dh and dx may each be h, dy or dh_in; at least one of dh, dx, gain_sums
  *   dh_in          [B * T, d] or NULL: the gradient that reaches h on the residual path
- *   gain_sums      device [B, d] fp32 or NULL; sums of a sample run in a fixed order
+ *   gain_sums      device [B, d] fp32 or NULL; sums of a sample run in a fixed order, long ones in pieces (T rows in one piece
+ *                  are off by about 2 sqrt(T) roundings at most, 256 at least)
  * d <= 16384, B * T < 2^31. */
 typedef struct {
   const void*  h;

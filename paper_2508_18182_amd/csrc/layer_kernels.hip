@@ -182,7 +182,8 @@ template <typename E, int NV, int WAVES, bool FAST> __global__ __launch_bounds__
 //   dh = dh_in + r (w - n mean(w n)),  dx = dropout(dh),  gain_sums[sample] = sum_t dy n.
 // Both sums of a row are formed in one pass, r again from h, which is here anyway.  A group of WAVES waves takes a run of one
 // sample's rows in order and keeps its columns of sum dy n in registers; runs are added up in order by a second kernel.
-// Rows whose sums leave fp32 make further passes over their registers.
+// Rows whose sums leave fp32 make further passes over their registers.  A long run puts its sums into memory every `piece` rows,
+// about the root of its length: rounding errors grow with that.
 // 32768 x 1024 bf16 with dh_in and dropout, 32 samples: 66 us, 5.1 TB/s, and 4.5 us for the runs (8 MB written and read again);
 // two rows ahead instead of one: the same (70.7 and 70.9 us in all), at 2048 columns worse (99 and 104).
 // ---------------------------------------------------------------------------------------------------------------------
@@ -197,6 +198,7 @@ struct NormBackArgs {
   long long hs, ys, is, os, xs;
   long long T;
   int runs;                  // per sample
+  int piece;                 // rows that are added up in registers, a power of two
   int d;
   float inv_d, eps;
   DropoutArgs m;
@@ -231,77 +233,87 @@ __global__ __launch_bounds__(64 * WAVES) void rms_norm_backward_kernel(NormBackA
   };
   constexpr bool ahead = NV < 4;                    // (wider rows have no registers left for it)
   if (ahead && first < last) fetch(first);
-  for (long long row = first; row < last; ++row) {
-    if (!ahead) fetch(row);
-    float h[NV][8], y[NV][8], in[NV][8];
+  long long row = first;
+  do {                                              // (once without a row: sums of nothing)
+    const long long end = last - row < a.piece ? last : row + a.piece;
+    for (; row < end; ++row) {
+      if (!ahead) fetch(row);
+      float h[NV][8], y[NV][8], in[NV][8];
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      widen_eight<E, FAST>(rh[i], c0 + i * 512 * WAVES, a.d, h[i]);
-      widen_eight<E, FAST>(ry[i], c0 + i * 512 * WAVES, a.d, y[i]);
-      if (a.dh_in) widen_eight<E, FAST>(ri[i], c0 + i * 512 * WAVES, a.d, in[i]);
-    }
-    if (ahead && row + 1 < last) fetch(row + 1);
-    float s[2] = {0.f, 0.f};
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        s[0] = fmaf(h[i][j], h[i][j], s[0]);
-        s[1] = fmaf(g[i][j] * y[i][j], h[i][j], s[1]);
+      for (int i = 0; i < NV; ++i) {
+        widen_eight<E, FAST>(rh[i], c0 + i * 512 * WAVES, a.d, h[i]);
+        widen_eight<E, FAST>(ry[i], c0 + i * 512 * WAVES, a.d, y[i]);
+        if (a.dh_in) widen_eight<E, FAST>(ri[i], c0 + i * 512 * WAVES, a.d, in[i]);
       }
-    row_sums<WAVES, 2>(s, lds, slot++ & 3);
-    float r = rsqrtf(fmaf(s[0], a.inv_d, a.eps)), mean = s[1] * r * a.inv_d, out = r;
-    // Sums that left fp32 (the same for the whole row).  w h may where w n does not: above it, or below it if r is large, when a
-    // sum of 0 may be one of lost products.
-    if (!(s[0] <= kLargest && fabsf(mean) <= kLargest && (r <= 1024.f || fabsf(s[1]) >= 0x1p-100f))) {
-      const float down = fabsf(s[1]) < 1.f ? 1.f : 0x1p-24f;         // w may be as large as fp32, and |n| adds up to d
-      if (!(s[0] <= kLargest)) {
+      if (ahead && row + 1 < last) fetch(row + 1);
+      float s[2] = {0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          s[0] = fmaf(h[i][j], h[i][j], s[0]);
+          s[1] = fmaf(g[i][j] * y[i][j], h[i][j], s[1]);
+        }
+      row_sums<WAVES, 2>(s, lds, slot++ & 3);
+      float r = rsqrtf(fmaf(s[0], a.inv_d, a.eps)), mean = s[1] * r * a.inv_d, out = r;
+      // Sums that left fp32 (the same for the whole row).  w h may where w n does not: above it, or below it if r is large, when a
+      // sum of 0 may be one of lost products.
+      if (!(s[0] <= kLargest && fabsf(mean) <= kLargest && (r <= 1024.f || fabsf(s[1]) >= 0x1p-100f))) {
+        const float down = fabsf(s[1]) < 1.f ? 1.f : 0x1p-24f;         // w may be as large as fp32, and |n| adds up to d
+        if (!(s[0] <= kLargest)) {
+          s[0] = s[1] = 0.f;
+#pragma unroll
+          for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              h[i][j] *= kTiny;
+              s[0] = fmaf(h[i][j], h[i][j], s[0]);
+            }
+          row_sums<WAVES, 2>(s, lds, slot++ & 3);
+          r = rsqrtf(fmaf(s[0], a.inv_d, float(double(a.eps) * (double(kTiny) * kTiny))));
+          out = r * kTiny;
+        }
         s[0] = s[1] = 0.f;
 #pragma unroll
         for (int i = 0; i < NV; ++i)
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            h[i][j] *= kTiny;
-            s[0] = fmaf(h[i][j], h[i][j], s[0]);
-          }
+          for (int j = 0; j < 8; ++j) s[1] = fmaf(g[i][j] * y[i][j] * down, h[i][j] * r, s[1]);
         row_sums<WAVES, 2>(s, lds, slot++ & 3);
-        r = rsqrtf(fmaf(s[0], a.inv_d, float(double(a.eps) * (double(kTiny) * kTiny))));
-        out = r * kTiny;
+        mean = s[1] * a.inv_d / down;
       }
-      s[0] = s[1] = 0.f;
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const int c = c0 + i * 512 * WAVES;
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float n = h[i][j] * r;
+          acc[i][j] = fmaf(y[i][j], n, acc[i][j]);
+          v[j] = out * fmaf(-n, mean, g[i][j] * y[i][j]);
+          if (a.dh_in) v[j] += in[i][j];
+        }
+        if (a.dh) store_eight<E, FAST>(static_cast<E*>(a.dh) + row * a.os, c, a.d, v);
+        if (a.dx) {
+          if (a.m.threshold) drop_eight(a.m, row, c, v);
+          store_eight<E, FAST>(static_cast<E*>(a.dx) + row * a.xs, c, a.d, v);
+        }
+      }
+    }
+    if (a.sums) {
+      const bool more = end - first > a.piece;        // there are sums of the pieces before
+      int at = c0;
+      asm volatile("" : "+v"(at));                    // (addresses formed here: kept through the rows, they cost their registers)
+      float* out = a.sums + (sample * a.runs + run) * a.d;
 #pragma unroll
       for (int i = 0; i < NV; ++i)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) s[1] = fmaf(g[i][j] * y[i][j] * down, h[i][j] * r, s[1]);
-      row_sums<WAVES, 2>(s, lds, slot++ & 3);
-      mean = s[1] * a.inv_d / down;
+        for (int j = 0; j < 8; ++j) {
+          const int c = at + i * 512 * WAVES + j;
+          if (c < a.d) out[c] = more ? out[c] + acc[i][j] : acc[i][j];
+          acc[i][j] = 0.f;
+        }
     }
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int c = c0 + i * 512 * WAVES;
-      float v[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float n = h[i][j] * r;
-        acc[i][j] = fmaf(y[i][j], n, acc[i][j]);
-        v[j] = out * fmaf(-n, mean, g[i][j] * y[i][j]);
-        if (a.dh_in) v[j] += in[i][j];
-      }
-      if (a.dh) store_eight<E, FAST>(static_cast<E*>(a.dh) + row * a.os, c, a.d, v);
-      if (a.dx) {
-        if (a.m.threshold) drop_eight(a.m, row, c, v);
-        store_eight<E, FAST>(static_cast<E*>(a.dx) + row * a.xs, c, a.d, v);
-      }
-    }
-  }
-  if (a.sums) {
-    float* out = a.sums + (sample * a.runs + run) * a.d;
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (c0 + i * 512 * WAVES + j < a.d) out[c0 + i * 512 * WAVES + j] = acc[i][j];
-  }
+  } while (row < last);
 }
 
 // Adds up a sample's runs: 64 columns per workgroup, a sixteenth of the runs per wave in order, then the sixteen in order.
@@ -600,6 +612,8 @@ extern "C" int adloco_rms_norm_backward(adloco_ctx* ctx, const adloco_norm_backw
   a.xs = m[4].stride;
   a.T = T;
   a.runs = int(runs);
+  a.piece = 256;
+  while ((long long)a.piece * a.piece < T / runs) a.piece *= 2;
   a.d = d;
   a.inv_d = float(1.0 / d);
   a.eps = float(eps);

@@ -199,3 +199,39 @@ def test_eps_counts_beside_large_rows(ctx, d):
     """eps 1e30 beside the smallest mean squares whose sum leaves fp32, 2.6e34 to 7.7e34: it moves the root by 100 to 300 u."""
     h = np.sign(normal(9, 3, d)) * np.sqrt(4.3e38 / d) * np.array([[1.0], [1.1], [1.2]])
     backward(ctx, h, None, normal(10, 3, d) * 1e10, 1e30)
+
+
+# ---- gain sums of long samples ----------------------------------------------------------------
+# A run of L rows is added up in pieces of p rows, p the power of two from 256 on whose square reaches L, the runs' sums in
+# sixteen parts: with values of one sign the sum is off by (p + L / p + runs / 16 + 16) u of itself, and 8 u for n and the products.
+
+def sums_of_one_sign(ctx, T, d, dtype, runs):
+    h = torch.ones(T, d, dtype=dtype, device=DEV)
+    h[:, 1::2] = -1
+    dy = torch.full((T, d), 0.1, dtype=dtype, device=DEV)
+    sums = torch.full((1, d), 9.0, device=DEV)
+    A.adloco_rms_norm_backward(ctx, h, None, dy, 1e-5, gain_sums=sums)
+    L, piece = -(-T // runs), 256
+    while piece * piece < L:
+        piece *= 2
+    want = T * float(dy[0, 0]) / np.sqrt(1 + 1e-5)
+    off = np.abs(host(sums)[0] * np.where(np.arange(d) % 2, -1, 1) - want)
+    assert off.max() <= (piece + L / piece + runs / 16 + 24) * U * want, off.max() / want
+    again = torch.empty_like(sums)
+    A.adloco_rms_norm_backward(ctx, h, None, dy, 1e-5, gain_sums=again)
+    assert torch.equal(again, sums)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,d", [(255, 8), (256, 9), (257, 8), (512, 24), (513, 8), (131149, 24), (70000, 1030), (66000, 8200)])
+def test_gain_sums_in_one_run(T, d, dtype):
+    """Without memory for scratch a sample is one run."""
+    ctx = A.Context(0)
+    ctx.set_tuning("scratch_limit_kb", 1)
+    sums_of_one_sign(ctx, T, d, TYPES[dtype], 1)
+    ctx.close()
+
+
+@pytest.mark.parametrize("T,d,waves", [((1 << 20) + 3, 520, 2), ((1 << 21) + 5, 2056, 8)])
+def test_gain_sums_of_a_long_sample(ctx, T, d, waves):
+    sums_of_one_sign(ctx, T, d, torch.bfloat16, 256 * (16 if d <= 1024 else 8) // waves)
