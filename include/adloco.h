@@ -525,7 +525,8 @@ int adloco_pack_blocks(adloco_ctx* ctx, const void* x, int64_t x_row_stride, int
  * (1.5e-5 of a sum of Gaussian values, a tenth of fp16's own rounding).  An fp32 output takes its operands as
  * bf16: what lies below 2^-133 (blocks of exponents 0 to 2) is rounded to a multiple of it, and 2^128 and
  * more (values above 3.29e38 before they were packed) is infinite.  A NaN in row m of a makes row m of out
- * NaN, one in row n of b column n; the exponent 255 is a block of NaN.  Rows are at most 2^23 bytes apart. */
+ * NaN, one in row n of b column n; the exponent 255 is a block of NaN.  Rows are at most 2^23 bytes apart, and out has at
+ * most 2^24 - 8 tiles of 128 x 128. */
 int adloco_block_product(adloco_ctx* ctx, const adloco_blocks8* a, const adloco_blocks8* b, void* out,
                          int64_t out_row_stride, int dtype, uint32_t flags, void* stream);
 

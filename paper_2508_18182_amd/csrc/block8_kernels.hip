@@ -35,7 +35,7 @@ struct PackArgs {
   long long rows, cols;
   unsigned char *q, *e, *qt, *et;      // along the rows, across them; NULL: not asked for
   long long qs, es, qts, ets;
-  unsigned col_tiles;
+  unsigned col_tiles, tiles;
 };
 
 constexpr int kPackThreads = 512, kPackRows = 4;
@@ -45,7 +45,9 @@ template <typename E, bool FAST> __global__ __launch_bounds__(kPackThreads) void
   __shared__ __attribute__((aligned(16))) unsigned most[128];
   __shared__ __attribute__((aligned(16))) unsigned turn[128][32];
   const int cg = threadIdx.x & 15, rg = threadIdx.x >> 4;
-  const long long rt = blockIdx.x / a.col_tiles, ct = blockIdx.x - rt * a.col_tiles;
+  const unsigned tile = unsigned(launch_index());
+  if (tile >= a.tiles) return;
+  const long long rt = tile / a.col_tiles, ct = tile - rt * a.col_tiles;
   const long long r0 = rt * 128 + rg * R, c0 = ct * 128;
   const int left = int(a.cols - c0 < 128 ? a.cols - c0 : 128);
   if (threadIdx.x < 128) most[threadIdx.x] = 0;
@@ -657,7 +659,9 @@ constexpr int kFewRows = 32;
 template <int RB, int WAVES, bool EXACT, typename E> __global__ __launch_bounds__(64 * WAVES) void product_few_kernel(ProductArgs p) {
   __shared__ float lds[WAVES][RB][4][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, kg = lane >> 4;
-  const int n = blockIdx.x * 16 + l16, nn = n < p.N ? n : p.N - 1;
+  const long long first = launch_index() * 16;
+  if (first >= p.N) return;
+  const int n = int(first) + l16, nn = n < p.N ? n : p.N - 1;
   const unsigned char* b = p.b + (long long)nn * p.bs + kg * 32;
   const unsigned char* eb = p.eb + nn;
   const unsigned char* a[RB];
@@ -725,8 +729,8 @@ template <int RB, int WAVES, bool EXACT, typename E> __global__ __launch_bounds_
 
 size_t size_of(int dtype) { return is_16bit(dtype) ? 2 : 4; }
 
-template <typename E, bool FAST> hipError_t launch_pack(const PackArgs& a, unsigned blocks, hipStream_t st) {
-  hipLaunchKernelGGL((pack_blocks_kernel<E, FAST>), dim3(blocks), dim3(kPackThreads), 0, st, a);
+template <typename E, bool FAST> hipError_t launch_pack(const PackArgs& a, hipStream_t st) {
+  hipLaunchKernelGGL((pack_blocks_kernel<E, FAST>), launch_grid(a.tiles, kPackThreads), dim3(kPackThreads), 0, st, a);
   return hipGetLastError();
 }
 template <int MB, int NB, bool WALK, typename E> hipError_t launch_tiles(const ProductArgs& p, hipStream_t st) {
@@ -746,9 +750,11 @@ template <int MB, int NB, bool WALK, typename E> hipError_t launch_tiles(const P
 int few_waves(long long N, long long steps) { return N > 255 * 16 && steps <= 64 ? 4 : 8; }
 template <int RB, typename E> hipError_t launch_few_rows(const ProductArgs& p, hipStream_t st) {
   constexpr bool exact = std::is_same<E, float>::value;
-  const unsigned blocks = unsigned(p.N + 15) / 16;
-  if (few_waves(p.N, p.steps) == 4) hipLaunchKernelGGL((product_few_kernel<RB, 4, exact, E>), dim3(blocks), dim3(256), 0, st, p);
-  else hipLaunchKernelGGL((product_few_kernel<RB, 8, exact, E>), dim3(blocks), dim3(512), 0, st, p);
+  const long long blocks = (p.N + 15LL) / 16;
+  if (few_waves(p.N, p.steps) == 4)
+    hipLaunchKernelGGL((product_few_kernel<RB, 4, exact, E>), launch_grid(blocks, 256), dim3(256), 0, st, p);
+  else
+    hipLaunchKernelGGL((product_few_kernel<RB, 8, exact, E>), launch_grid(blocks, 512), dim3(512), 0, st, p);
   return hipGetLastError();
 }
 template <typename E> hipError_t launch_few(const ProductArgs& p, hipStream_t st) {
@@ -858,6 +864,7 @@ extern "C" int adloco_pack_blocks(adloco_ctx* ctx, const void* x, int64_t x_row_
   a.rows = rows;
   a.cols = cols;
   a.col_tiles = unsigned(ct);
+  a.tiles = unsigned(rt * ct);
   if (along) {
     a.q = static_cast<unsigned char*>(along->data);
     a.e = along->exponent;
@@ -874,12 +881,11 @@ extern "C" int adloco_pack_blocks(adloco_ctx* ctx, const void* x, int64_t x_row_
   DeviceScope scope(ctx);
   if (!scope.ok()) return fail(ctx, ADLOCO_EHIP, "pack_blocks: device %d cannot be made current", ctx->device);
   hipStream_t st = static_cast<hipStream_t>(stream);
-  const unsigned n = unsigned(rt * ct);
   hipEvent_t ev = prof_begin(ctx, st);
   hipError_t e;
-  if (dtype == ADLOCO_BF16) e = fast ? launch_pack<__bf16, true>(a, n, st) : launch_pack<__bf16, false>(a, n, st);
-  else if (dtype == ADLOCO_F16) e = fast ? launch_pack<_Float16, true>(a, n, st) : launch_pack<_Float16, false>(a, n, st);
-  else e = fast ? launch_pack<float, true>(a, n, st) : launch_pack<float, false>(a, n, st);
+  if (dtype == ADLOCO_BF16) e = fast ? launch_pack<__bf16, true>(a, st) : launch_pack<__bf16, false>(a, st);
+  else if (dtype == ADLOCO_F16) e = fast ? launch_pack<_Float16, true>(a, st) : launch_pack<_Float16, false>(a, st);
+  else e = fast ? launch_pack<float, true>(a, st) : launch_pack<float, false>(a, st);
   prof_end(ctx, kProfPack, ev, st);
   if (e != hipSuccess) return fail(ctx, ADLOCO_EHIP, "pack_blocks launch failed: %s", hipGetErrorString(e));
   return ADLOCO_OK;
@@ -935,7 +941,7 @@ extern "C" int adloco_block_product(adloco_ctx* ctx, const adloco_blocks8* a, co
   }
   const bool few = c.kernel == 1, large = c.kernel == 8;
   const int64_t edge = large ? 256 : 128, tm = (a->rows + edge - 1) / edge, tn = (b->rows + edge - 1) / edge;
-  if (tm * tn > 0xffffffLL) return fail(ctx, ADLOCO_EUNSUPPORTED, "block_product: too many tiles for one launch");
+  if (tm * tn > 0xfffff8LL) return fail(ctx, ADLOCO_EUNSUPPORTED, "block_product: too many tiles for one launch");
   p.tiles_m = int(tm);
   p.tiles_n = int(tn);
   p.pieces = c.pieces;

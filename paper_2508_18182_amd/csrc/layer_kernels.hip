@@ -24,7 +24,7 @@ struct DropArgs {
 };
 
 template <typename E, bool FAST> __global__ __launch_bounds__(64) void dropout_kernel(DropArgs a) {
-  const long long i = (long long)blockIdx.x * 64 + threadIdx.x;
+  const long long i = launch_index() * 64 + threadIdx.x;
   if (i >= a.total) return;
   const long long row = a.total <= 0xffffffffLL ? unsigned(i) / a.per_row : i / a.per_row;
   const int c = int(i - row * a.per_row) * 8;
@@ -198,6 +198,7 @@ struct NormBackArgs {
   long long hs, ys, is, os, xs;
   long long T;
   int runs;                  // per sample
+  unsigned groups;           // samples * runs
   int piece;                 // rows that are added up in registers, a power of two
   int d;
   float inv_d, eps;
@@ -209,8 +210,10 @@ __global__ __launch_bounds__(64 * WAVES) void rms_norm_backward_kernel(NormBackA
   __shared__ float lds[4][8][2];
   int slot = 0;
   const int c0 = threadIdx.x * 8;
-  const long long sample = blockIdx.x / a.runs;
-  const int run = int(blockIdx.x - sample * a.runs);
+  const unsigned group = unsigned(launch_index());
+  if (group >= a.groups) return;
+  const long long sample = group / unsigned(a.runs);
+  const int run = int(group - sample * a.runs);
   const long long first = sample * a.T + a.T * run / a.runs, last = sample * a.T + a.T * (run + 1) / a.runs;
   float acc[NV][8], g[NV][8];
   const bool gain_vec = reinterpret_cast<unsigned long long>(a.gain) % 16 == 0;
@@ -404,7 +407,7 @@ template <template <typename, bool> class F, typename... A> hipError_t by_type(i
 
 template <typename E, bool FAST> struct LaunchDropout {
   static hipError_t run(const DropArgs& a, hipStream_t st) {
-    hipLaunchKernelGGL((dropout_kernel<E, FAST>), dim3(unsigned((a.total + 63) / 64)), dim3(64), 0, st, a);
+    hipLaunchKernelGGL((dropout_kernel<E, FAST>), launch_grid((a.total + 63) / 64, 64), dim3(64), 0, st, a);
     return hipGetLastError();
   }
 };
@@ -429,7 +432,9 @@ template <typename E, bool FAST> struct LaunchNorm {
     // as others end (at once / dealt out: 32768 x 2048 110 / 103 us, 32768 x 768 with dropout 51 / 46, one row each 107 / 49; at
     // five rows, 2500 x 5000, at once 26, dealt out 27).
     const long long most = (long long)kNumCu * 16 / norm_waves(a.wide);
-    const dim3 grid(unsigned(a.rows < most ? a.rows : a.rows < 8 * most ? most : (a.rows + 3) / 4));
+    const long long groups = a.rows < most ? a.rows : a.rows < 8 * most ? most : (a.rows + 3) / 4;
+    const long long limit = 0xffffffffLL / (64 * norm_waves(a.wide));      // (a launch holds fewer than 2^32 work items)
+    const dim3 grid(unsigned(groups < limit ? groups : limit));
 #define ADLOCO_CALL(NV, WAVES) hipLaunchKernelGGL((rms_norm_kernel<E, NV, WAVES, FAST>), grid, dim3(64 * WAVES), 0, st, a)
     ADLOCO_NORM_SHAPE(a.wide, ADLOCO_CALL);
 #undef ADLOCO_CALL
@@ -438,9 +443,9 @@ template <typename E, bool FAST> struct LaunchNorm {
 };
 
 template <typename E, bool FAST> struct LaunchNormBack {
-  static hipError_t run(const NormBackArgs& a, unsigned groups, hipStream_t st) {
+  static hipError_t run(const NormBackArgs& a, hipStream_t st) {
 #define ADLOCO_CALL(NV, WAVES) \
-  hipLaunchKernelGGL((rms_norm_backward_kernel<E, NV, WAVES, FAST>), dim3(groups), dim3(64 * WAVES), 0, st, a)
+  hipLaunchKernelGGL((rms_norm_backward_kernel<E, NV, WAVES, FAST>), launch_grid(a.groups, 64 * WAVES), dim3(64 * WAVES), 0, st, a)
     ADLOCO_NORM_SHAPE(a.d, ADLOCO_CALL);
 #undef ADLOCO_CALL
     return hipGetLastError();
@@ -621,7 +626,8 @@ extern "C" int adloco_rms_norm_backward(adloco_ctx* ctx, const adloco_norm_backw
   if (B * runs > 0x7fffffffLL || (runs > 1 && B * slabs > 0x7fffffffLL))
     return fail(ctx, ADLOCO_EUNSUPPORTED, "rms_norm_backward: too many samples for one launch");
   hipEvent_t ev = prof_begin(ctx, st);
-  hipError_t e = by_type<LaunchNormBack>(dtype, fast, a, unsigned(B * runs), st);
+  a.groups = unsigned(B * runs);
+  hipError_t e = by_type<LaunchNormBack>(dtype, fast, a, st);
   if (e == hipSuccess && io->gain_sums && runs > 1) {
     hipLaunchKernelGGL(gain_runs_kernel, dim3(unsigned(B * slabs)), dim3(64 * kRunWaves), 0, st, parts, int(runs), d, slabs, io->gain_sums);
     e = hipGetLastError();

@@ -7,6 +7,9 @@
 
 namespace adloco {
 
+// Number of a workgroup in a grid of launch_grid.
+__device__ __forceinline__ long long launch_index() { return (long long)blockIdx.y * gridDim.x + blockIdx.x; }
+
 // ---- eight consecutive values of a row -----------------------------------------------------------------------------
 // FAST: rows are 16-byte aligned and whole multiples of eight long, so that a lane's eight are all there or all not.
 // Others are loaded eight at a time all the same, at element alignment: the last ones of a row as the last eight, moved down
@@ -237,6 +240,13 @@ class DeviceScope {
   int before_ = -1;
   bool ok_ = true;
 };
+
+// Grid of n workgroups: a launch holds fewer than 2^32 work items in a dimension, so many small workgroups take a second one.
+// The last ones, from launch_index() >= n on, have nothing to do.
+inline dim3 launch_grid(long long n, int threads) {
+  const long long most = 0xffffffffLL / threads, y = (n + most - 1) / most;
+  return y <= 1 ? dim3(unsigned(n)) : dim3(unsigned((n + y - 1) / y), unsigned(y));
+}
 
 // One matrix argument as the checks see it: `rows` rows of `width` bytes, `stride` bytes apart.
 struct RowSpan {
