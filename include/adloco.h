@@ -520,13 +520,14 @@ int adloco_pack_blocks(adloco_ctx* ctx, const void* x, int64_t x_row_stride, int
  * (a.cols == b.cols).  With activations x8 [T, d_in] and W8 [d_out, d_in] the layer's output; with
  * delta8 [T, d_out] and W packed across [d_in, d_out] the input gradient; with delta and x packed across
  * ([d_out, T] and [d_in, T]) the gradient sum, fp32, with ADLOCO_ACCUMULATE added to what is there.
- * Only an fp32 output accumulates.  Sums are fp32 and rounded once at the end; products are exact for fp32
- * outputs, while for 16-bit ones the 8-bit instruction cuts each off below 2^-13 of the largest of its group
- * (1.5e-5 of a sum of Gaussian values, a tenth of fp16's own rounding).  An fp32 output takes its operands as
- * bf16: what lies below 2^-133 (blocks of exponents 0 to 2) is rounded to a multiple of it, and 2^128 and
- * more (values above 3.29e38 before they were packed) is infinite.  A NaN in row m of a makes row m of out
- * NaN, one in row n of b column n; the exponent 255 is a block of NaN.  Rows are at most 2^23 bytes apart, and out has at
- * most 2^24 - 8 tiles of 128 x 128. */
+ * Only an fp32 output accumulates.  Sums are fp32 and rounded once at the end.  Products are exact for fp32
+ * outputs and for few rows (up to 32 of a, unless the contraction is so long for its columns that tiles are the
+ * faster kernel).  For other 16-bit outputs the 8-bit instruction cuts each off below 2^-13 of the largest of its
+ * group: 1.5e-5 of a sum of Gaussian values, a tenth of fp16's own rounding, but products that cancel leave that
+ * much of their own size.  Exact products take their operands as bf16: what lies below 2^-133 (blocks of exponents
+ * 0 to 2) is rounded to a multiple of it, and 2^128 and more (values above 3.29e38 before they were packed) is
+ * infinite.  A NaN in row m of a makes row m of out NaN, one in row n of b column n; the exponent 255 is a block of
+ * NaN.  Rows are at most 2^23 bytes apart, and out has at most 2^24 - 8 tiles of 128 x 128. */
 int adloco_block_product(adloco_ctx* ctx, const adloco_blocks8* a, const adloco_blocks8* b, void* out,
                          int64_t out_row_stride, int dtype, uint32_t flags, void* stream);
 

@@ -652,11 +652,13 @@ template <int EDGE_M, int EDGE_N, typename E> __global__ __launch_bounds__(256) 
 // ---------------------------------------------------------------------------------------------------------------------
 // Few rows of A (up to 32): B is read once, by whoever multiplies it, straight into registers; all else is latency.  A
 // workgroup takes 16 columns, its waves share the blocks of k among them and add up what they have through LDS, in order.
-// 3 x 5632 x 2048: 5.2 us (on small tiles 11), 2.2 TB/s of B; 33 to 64 rows would take 13 us, on small tiles 10.
+// 3 x 5632 x 2048: 5.2 us (on small tiles 11), 2.2 TB/s of B; 33 to 64 rows would take 13 us, on small tiles 10.  Widened like
+// fp32 outputs whatever the output is: the vector and matrix cores wait for memory anyway (8-bit instruction / widened:
+// 3 x 5632 x 2048 7.0 / 7.0 us with the host, 32 x 8192 x 8192 24.9 / 25.3, 8 x 4096 x 14336 15.0 / 15.4).
 // ---------------------------------------------------------------------------------------------------------------------
 constexpr int kFewRows = 32;
 
-template <int RB, int WAVES, bool EXACT, typename E> __global__ __launch_bounds__(64 * WAVES) void product_few_kernel(ProductArgs p) {
+template <int RB, int WAVES, typename E> __global__ __launch_bounds__(64 * WAVES) void product_few_kernel(ProductArgs p) {
   __shared__ float lds[WAVES][RB][4][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, kg = lane >> 4;
   const long long first = launch_index() * 16;
@@ -696,17 +698,12 @@ template <int RB, int WAVES, bool EXACT, typename E> __global__ __launch_bounds_
 #pragma unroll
     for (int i = 0; i < U; ++i) {
       if (s0 + i * WAVES >= p.steps) break;           // (the same for the wave)
-      WideFrag wb;
-      if constexpr (EXACT) wb = widen(fb[i], unsigned(xb[i]));
+      const WideFrag wb = widen(fb[i], unsigned(xb[i]));
 #pragma unroll
       for (int r = 0; r < RB; ++r) {
-        if constexpr (EXACT) {
-          const WideFrag wa = widen(fa[i][r], unsigned(xa[i][r]));
+        const WideFrag wa = widen(fa[i][r], unsigned(xa[i][r]));
 #pragma unroll
-          for (int k = 0; k < 4; ++k) acc[r] = mfma_16x16x32_v<false>(wa.k[k], wb.k[k], acc[r]);
-        } else {
-          scaled_mfma<0, 0, false, false>(acc[r], fa[i][r], fb[i], xa[i][r], xb[i]);
-        }
+        for (int k = 0; k < 4; ++k) acc[r] = mfma_16x16x32_v<false>(wa.k[k], wb.k[k], acc[r]);
       }
     }
   }
@@ -749,12 +746,11 @@ template <int MB, int NB, bool WALK, typename E> hipError_t launch_tiles(const P
 // Waves per workgroup: as many blocks of k under way as it takes to fill the chip.
 int few_waves(long long N, long long steps) { return N > 255 * 16 && steps <= 64 ? 4 : 8; }
 template <int RB, typename E> hipError_t launch_few_rows(const ProductArgs& p, hipStream_t st) {
-  constexpr bool exact = std::is_same<E, float>::value;
   const long long blocks = (p.N + 15LL) / 16;
   if (few_waves(p.N, p.steps) == 4)
-    hipLaunchKernelGGL((product_few_kernel<RB, 4, exact, E>), launch_grid(blocks, 256), dim3(256), 0, st, p);
+    hipLaunchKernelGGL((product_few_kernel<RB, 4, E>), launch_grid(blocks, 256), dim3(256), 0, st, p);
   else
-    hipLaunchKernelGGL((product_few_kernel<RB, 8, exact, E>), launch_grid(blocks, 512), dim3(512), 0, st, p);
+    hipLaunchKernelGGL((product_few_kernel<RB, 8, E>), launch_grid(blocks, 512), dim3(512), 0, st, p);
   return hipGetLastError();
 }
 template <typename E> hipError_t launch_few(const ProductArgs& p, hipStream_t st) {
