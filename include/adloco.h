@@ -62,6 +62,7 @@ extern "C" {
 #define ADLOCO_ACCUMULATE       0x1u  /* grad_stats: continue a batch (switch mode micro-batch);
                                          block_product: add to the output                        */
 #define ADLOCO_SUM_ONLY         0x2u  /* grad_stats: form the gradient sums only, no norms       */
+#define ADLOCO_EXACT_PRODUCTS   0x4u  /* block_product: exact products for 16-bit outputs too    */
 #define ADLOCO_GRAD_PROVIDED    0x1u  /* linear_desc.flags: caller maintains grad_sum itself     */
 /* linear_desc.flags, bits 4..7: which block of the parameters the descriptor stands for      */
 #define ADLOCO_KIND_LINEAR      0x00u /* weight W [d_out, d_in] of a linear layer (the default)  */
@@ -524,7 +525,8 @@ int adloco_pack_blocks(adloco_ctx* ctx, const void* x, int64_t x_row_stride, int
  * outputs and for few rows (up to 32 of a, unless the contraction is so long for its columns that tiles are the
  * faster kernel).  For other 16-bit outputs the 8-bit instruction cuts each off below 2^-13 of the largest of its
  * group: 1.5e-5 of a sum of Gaussian values, a tenth of fp16's own rounding, but products that cancel leave that
- * much of their own size.  Exact products take their operands as bf16: what lies below 2^-133 (blocks of exponents
+ * much of their own size.  ADLOCO_EXACT_PRODUCTS makes those exact as well, in about twice the time.
+ * Exact products take their operands as bf16: what lies below 2^-133 (blocks of exponents
  * 0 to 2) is rounded to a multiple of it, and 2^128 and more (values above 3.29e38 before they were packed) is
  * infinite.  A NaN in row m of a makes row m of out NaN, one in row n of b column n; the exponent 255 is a block of
  * NaN.  Rows are at most 2^23 bytes apart, and out has at most 2^24 - 8 tiles of 128 x 128. */

@@ -15,6 +15,7 @@ _LIB_PATH = os.environ.get("ADLOCO_LIBRARY_PATH") or os.path.join(_PKG, "libadlo
 ADLOCO_F32, ADLOCO_BF16, ADLOCO_F16 = 0, 1, 2
 ADLOCO_ACCUMULATE = 0x1
 ADLOCO_SUM_ONLY = 0x2
+ADLOCO_EXACT_PRODUCTS = 0x4
 ADLOCO_GRAD_PROVIDED = 0x1
 ADLOCO_KIND_LINEAR, ADLOCO_KIND_VECTOR, ADLOCO_KIND_EMBED, ADLOCO_KIND_SAMPLE_SUMS = 0x00, 0x10, 0x20, 0x40
 ADLOCO_KIND_MASK = 0xF0
@@ -744,7 +745,8 @@ def adloco_pack_blocks(ctx: Context, x, along: Optional[Blocks8] = None, across:
 
 
 def adloco_block_product(ctx: Context, a: Blocks8, b: Blocks8, out, flags: int = 0, stream=None):
-    """out [a.rows, b.rows] (fp32, bf16 or fp16) = a b^T; with ADLOCO_ACCUMULATE (fp32) added to out."""
+    """out [a.rows, b.rows] (fp32, bf16 or fp16) = a b^T; with ADLOCO_ACCUMULATE (fp32) added to out.  Products for 16-bit
+    outputs are cut off below 2^-13 of the largest of their group unless flags hold ADLOCO_EXACT_PRODUCTS."""
     shape = out.shape
     code = _layer_dtype(out.dtype, "out")
     da, db = _blocks8(ctx, a, "a"), _blocks8(ctx, b, "b")

@@ -169,8 +169,9 @@ template <typename E, bool FAST> __global__ __launch_bounds__(kPackThreads) void
 // two powers of two by itself.  It adds its products in groups whose members it cuts off below 2^-13 of the largest of them
 // (measured; the unscaled 8-bit instructions do the same), which leaves 1.5e-5 of a sum of Gaussian values: a hundredth of
 // what the output's own rounding costs in bf16, a tenth in fp16.
-//   fp32 outputs (EXACT): gradient sums would keep that error, so the values are widened to bf16 in registers, where they and
-// their powers of two are exact, and multiplied by v_mfma_f32_16x16x32_bf16 at half the rate: products exact, sums fp32.
+//   fp32 outputs, and 16-bit ones by request (EXACT): gradient sums would keep that error, so the values are widened to bf16 in
+// registers, where they and their powers of two are exact, and multiplied by v_mfma_f32_16x16x32_bf16 at half the rate: products
+// exact, sums fp32.
 // Which 32 of the 128 values of k a lane holds does not matter as long as both operands agree; which 16 rows make a block of
 // the tile is free too, and a lane takes neighbouring rows for the blocks (row = lane * NB + block), so that their exponents
 // are one load and a lane's outputs of a row one store.
@@ -730,10 +731,9 @@ template <typename E, bool FAST> hipError_t launch_pack(const PackArgs& a, hipSt
   hipLaunchKernelGGL((pack_blocks_kernel<E, FAST>), launch_grid(a.tiles, kPackThreads), dim3(kPackThreads), 0, st, a);
   return hipGetLastError();
 }
-template <int MB, int NB, bool WALK, typename E> hipError_t launch_tiles(const ProductArgs& p, hipStream_t st) {
-  constexpr bool exact = std::is_same<E, float>::value;
-  using T = TileShape<MB, NB, exact>;
-  auto kern = product_tile_kernel<MB, NB, exact, WALK, E>;
+template <int MB, int NB, bool EXACT, bool WALK, typename E> hipError_t launch_tiles(const ProductArgs& p, hipStream_t st) {
+  using T = TileShape<MB, NB, EXACT>;
+  auto kern = product_tile_kernel<MB, NB, EXACT, WALK, E>;
   const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, T::lds);
   if (e != hipSuccess) return e;
   const unsigned total = unsigned(p.tiles_m) * unsigned(p.tiles_n);
@@ -758,24 +758,26 @@ template <typename E> hipError_t launch_few(const ProductArgs& p, hipStream_t st
 }
 // More large tiles than compute units, whole, of an even number of blocks: one workgroup per compute unit walks over them (one
 // workgroup per tile / walking: 32768 x 5632 x 2048 357 / 342 us, x 512 118 / 114, 8192 x 8192 x 1024 66 / 64).
-template <typename E> hipError_t launch_product(const ProductArgs& p, bool large, hipStream_t st) {
-  if constexpr (!std::is_same<E, float>::value)
+template <typename E> hipError_t launch_product(const ProductArgs& p, bool large, bool exact, hipStream_t st) {
+  if constexpr (!std::is_same<E, float>::value) {
     if (large) {
       const bool walk = p.pieces == 1 && p.steps % 2 == 0 && p.tiles_m * p.tiles_n > kNumCu;
-      return walk ? launch_tiles<8, 8, true, E>(p, st) : launch_tiles<8, 8, false, E>(p, st);
+      return walk ? launch_tiles<8, 8, false, true, E>(p, st) : launch_tiles<8, 8, false, false, E>(p, st);
     }
-  return launch_tiles<4, 4, false, E>(p, st);
+    if (!exact) return launch_tiles<4, 4, false, false, E>(p, st);
+  }
+  return launch_tiles<4, 4, true, false, E>(p, st);
 }
 
 // Which kernel, and how many pieces the contraction is cut into.  Times in microseconds, fitted to 5600 timings over 250
 // shapes (1 to 32768 rows, 64 to 8192 columns, 128 to 32768 values of k; log error 13 %): 0.36 a block of k for a small tile
-// that has its compute unit to itself and 0.95 for two that share it (fp32 outputs 0.75 and 1.5), 0.93 for a large tile, 3.0
+// that has its compute unit to itself and 0.95 for two that share it (exact products 0.75 and 1.5), 0.93 for a large tile, 3.0
 // and 6.5 to start and store one; 1.7 and the partial tiles' way out and back for a second kernel.  The choice is within 4 %
 // of the best one on average.  Measured, few rows / small tiles / small tiles in 4 pieces / large: 3 x 5632 x 2048 7 / 11 / 11
 // / 23, 64 x 8192 x 8192 - / 29 / 20 / 60, 512 x 5632 x 2048 - / 15 / 26 / 35, 32768 x 5632 x 2048 - / 376 / - / 300 us.
 // Rows of the output that are not 16-byte aligned count 12 us more for a large tile (32001 x 2044 x 1024: small 78, large 104).
 struct ProductChoice { int kernel, pieces; };          // kernel: 1 few rows, 4 small tiles, 8 large ones
-ProductChoice choose_product(long long M, long long N, int steps, bool fp32, bool aligned, int kernel, int pieces, bool split) {
+ProductChoice choose_product(long long M, long long N, int steps, bool exact, bool aligned, int kernel, int pieces, bool split) {
   ProductChoice best{4, 1};
   double least = 1e300;
   auto offer = [&](int k, int n, double t) {
@@ -790,7 +792,7 @@ ProductChoice choose_product(long long M, long long N, int steps, bool fp32, boo
     offer(1, 1, 1.2 + double((steps + waves - 1) / waves) * (share > 1.0 ? share : 1.0) * (M <= 16 ? 0.45 : 0.65));
   }
   for (int k = 4; k <= 8; k += 4) {
-    if ((kernel > 1 && k != kernel && !(fp32 && k == 4)) || (fp32 && k == 8)) continue;
+    if ((kernel > 1 && k != kernel && !(exact && k == 4)) || (exact && k == 8)) continue;
     const long long edge = 32 * k, tiles = ((M + edge - 1) / edge) * ((N + edge - 1) / edge);
     const int most = !split ? 1 : pieces ? pieces : 64;
     for (int p = pieces && split ? pieces : 1; p <= most; ++p) {
@@ -802,7 +804,7 @@ ProductChoice choose_product(long long M, long long N, int steps, bool fp32, boo
       const double w = double(tiles) * n, s = double((steps + n - 1) / n);
       double t;
       if (k == 4) {
-        const double alone = s * (fp32 ? 0.75 : 0.36) + 3.0, shared = s * (fp32 ? 1.5 : 0.95) + 3.0;
+        const double alone = s * (exact ? 0.75 : 0.36) + 3.0, shared = s * (exact ? 1.5 : 0.95) + 3.0;
         const double full = double((long long)w / (2 * kNumCu)), left = w - full * 2 * kNumCu;
         t = full * shared + (left > kNumCu ? shared : left > 0 ? alone : 0.0);
       } else {
@@ -892,7 +894,7 @@ extern "C" int adloco_block_product(adloco_ctx* ctx, const adloco_blocks8* a, co
   if (!ctx) return ADLOCO_EINVAL;
   if (dtype != ADLOCO_F32 && !is_16bit(dtype)) return fail(ctx, ADLOCO_EUNSUPPORTED, "block_product: dtype %d not supported", dtype);
   if (!a || !b) return fail(ctx, ADLOCO_EINVAL, "block_product: a or b is NULL");
-  if (flags & ~ADLOCO_ACCUMULATE) return fail(ctx, ADLOCO_EINVAL, "block_product: unknown flags");
+  if (flags & ~(ADLOCO_ACCUMULATE | ADLOCO_EXACT_PRODUCTS)) return fail(ctx, ADLOCO_EINVAL, "block_product: unknown flags");
   if ((flags & ADLOCO_ACCUMULATE) && dtype != ADLOCO_F32)
     return fail(ctx, ADLOCO_EUNSUPPORTED, "block_product: only an fp32 output accumulates");
   if (const char* why = check_blocks8(a)) return fail(ctx, ADLOCO_EINVAL, "block_product: a: %s", why);
@@ -928,12 +930,12 @@ extern "C" int adloco_block_product(adloco_ctx* ctx, const adloco_blocks8* a, co
   DeviceScope scope(ctx);
   if (!scope.ok()) return fail(ctx, ADLOCO_EHIP, "block_product: device %d cannot be made current", ctx->device);
   hipStream_t st = static_cast<hipStream_t>(stream);
-  const bool fp32 = dtype == ADLOCO_F32;
+  const bool exact = dtype == ADLOCO_F32 || (flags & ADLOCO_EXACT_PRODUCTS);
   const bool aligned = reinterpret_cast<uintptr_t>(out) % 16 == 0 && os * (int64_t)es % 16 == 0;
-  ProductChoice c = choose_product(a->rows, b->rows, p.steps, fp32, aligned, ctx->product_blocks, ctx->product_pieces, true);
+  ProductChoice c = choose_product(a->rows, b->rows, p.steps, exact, aligned, ctx->product_blocks, ctx->product_pieces, true);
   if (c.pieces > 1) {
     p.part = layer_scratch(ctx, st);
-    if (!p.part) c = choose_product(a->rows, b->rows, p.steps, fp32, aligned, ctx->product_blocks, ctx->product_pieces, false);
+    if (!p.part) c = choose_product(a->rows, b->rows, p.steps, exact, aligned, ctx->product_blocks, ctx->product_pieces, false);
   }
   const bool few = c.kernel == 1, large = c.kernel == 8;
   const int64_t edge = large ? 256 : 128, tm = (a->rows + edge - 1) / edge, tn = (b->rows + edge - 1) / edge;
@@ -946,8 +948,8 @@ extern "C" int adloco_block_product(adloco_ctx* ctx, const adloco_blocks8* a, co
   hipEvent_t ev = prof_begin(ctx, st);
   const hipError_t e = few ? (dtype == ADLOCO_BF16 ? launch_few<__bf16>(p, st) : dtype == ADLOCO_F16 ? launch_few<_Float16>(p, st)
                                                                                   : launch_few<float>(p, st))
-                       : dtype == ADLOCO_BF16 ? launch_product<__bf16>(p, large, st)
-                       : dtype == ADLOCO_F16 ? launch_product<_Float16>(p, large, st) : launch_product<float>(p, large, st);
+                       : dtype == ADLOCO_BF16 ? launch_product<__bf16>(p, large, exact, st)
+                       : dtype == ADLOCO_F16 ? launch_product<_Float16>(p, large, exact, st) : launch_product<float>(p, large, exact, st);
   prof_end(ctx, kProfProduct, ev, st);
   if (e != hipSuccess) return fail(ctx, ADLOCO_EHIP, "block_product launch failed: %s", hipGetErrorString(e));
   return ADLOCO_OK;

@@ -59,6 +59,62 @@ def test_few_rows_by_the_sizes(ctx, m, n, k):
     assert torch.equal(out.cpu(), torch.from_numpy(want).to(torch.bfloat16))
 
 
+# (16 x 16 blocks per wave and side, pieces of the contraction); 0: the library's choice
+@pytest.mark.parametrize("variant", [(0, 0), (1, 0), (4, 1), (4, 3), (8, 1), (8, 7)], ids=lambda v: f"{v[0]}x{v[1]}")
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("m,n,k", [(1, 1, 2), (20, 70, 300), (33, 129, 1000), (128, 128, 128), (130, 1000, 250), (300, 513, 4000), (257, 260, 9000)])
+def test_by_request(ctx, m, n, k, dtype, variant):
+    """ADLOCO_EXACT_PRODUCTS, whatever the kernel: rows that are aligned and rows that are not, nothing between them."""
+    a, b, want = cancelling(m, n, k)
+    ctx.set_tuning("product_blocks", variant[0])
+    ctx.set_tuning("product_pieces", variant[1])
+    try:
+        for pad in (0, 3, 8):
+            buf = torch.full((m, n + pad), 7.0, dtype=TYPES[dtype], device=DEV)
+            A.adloco_block_product(ctx, blocks(a), blocks(b), buf[:, :n], A.ADLOCO_EXACT_PRODUCTS)
+            assert torch.equal(buf[:, :n].cpu(), torch.from_numpy(want).to(TYPES[dtype]))
+            assert bool((buf[:, n:] == 7).all())
+        if dtype == "f32":
+            out = torch.full((m, n), 5.0, device=DEV)
+            A.adloco_block_product(ctx, blocks(a), blocks(b), out, A.ADLOCO_EXACT_PRODUCTS | A.ADLOCO_ACCUMULATE)
+            assert torch.equal(out.cpu(), torch.from_numpy(want + 5).float())
+    finally:
+        ctx.set_tuning("product_blocks", 0)
+        ctx.set_tuning("product_pieces", 0)
+
+
+@pytest.mark.parametrize("m,n,k", [(4200, 4100, 1024), (65281, 256, 512)])
+def test_large_outputs_by_request(ctx, m, n, k):
+    a, b, _ = cancelling(m, n, k)
+    out = torch.empty((m, n), dtype=torch.bfloat16, device=DEV)
+    A.adloco_block_product(ctx, blocks(a), blocks(b), out, A.ADLOCO_EXACT_PRODUCTS)
+    want = torch.from_numpy(a).to(DEV) @ torch.from_numpy(b).to(DEV).T.contiguous()
+    assert torch.equal(out, want.to(torch.bfloat16))
+
+
+@pytest.mark.parametrize("variant", [(4, 1), (4, 3), (8, 1), (8, 2)], ids=lambda v: f"{v[0]}x{v[1]}")
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("m,n,k", [(33, 129, 1000), (300, 260, 2000)])
+def test_what_the_8_bit_instruction_leaves(ctx, m, n, k, dtype, variant):
+    """Without it: each product is cut off below 2^-13 of the largest of a group of at most 32, so that a group is off by 32 times
+    2^-13 of its largest product, and all of them by that of the sum of their largest ones: the pairs of 448 lie in six groups at
+    most, every other group's products are 64 at most."""
+    a, b, want = cancelling(m, n, k)
+    ctx.set_tuning("product_blocks", variant[0])
+    ctx.set_tuning("product_pieces", variant[1])
+    try:
+        out = torch.empty((m, n), dtype=TYPES[dtype], device=DEV)
+        A.adloco_block_product(ctx, blocks(a), blocks(b), out)
+    finally:
+        ctx.set_tuning("product_blocks", 0)
+        ctx.set_tuning("product_pieces", 0)
+    largest = 6 * 448.0**2 + 64.0 * (-(-k // 128) * 128 // 32 * 4)              # (groups of eight at least)
+    half = torch.finfo(TYPES[dtype]).eps / 2
+    off = np.abs(out.cpu().double().numpy() - want)
+    cut = 32 * 2.0**-13 * largest
+    assert (off <= half * np.abs(want) + cut * (1 + half)).all()
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("ea,eb,top", [(0, 200, 448), (1, 200, 448), (2, 230, 448), (3, 200, 448), (200, 1, 448), (246, 60, 448),
                                        (60, 246, 448), (247, 60, 240), (254, 20, 1.75), (3, 246, 448), (255, 127, 448)])
