@@ -540,7 +540,7 @@ int adloco_block_product(adloco_ctx* ctx, const adloco_blocks8* a, const adloco_
  *   gain        device [d] fp32, or NULL for ones
  *   mask        NULL or p = 0: no dropout
  *   y8          y in 8-bit blocks (rounded from fp32), or NULL; at least one of h, y, y8
- * d <= 16384; eps a positive normal fp32 number. */
+ * d <= 16384; eps a positive normal fp32 number, at most 1e30. */
 typedef struct {
   const void*  x;
   const void*  residual;
