@@ -432,7 +432,8 @@ typedef struct {
 /* Runs the model of worker `worker` of the trainer that owns `user` at parameters `theta`
  * (device) on `b` fresh samples and describes the result: on entry layers[l] holds d_in, d_out,
  * grad_sum, flags of the template; the callback fills a, delta and the row strides (device
- * tensors [b, T, .] that stay valid until the next callback for this trainer), and for blocks
+ * tensors [b, T, .], for ADLOCO_KIND_SAMPLE_SUMS delta = fp32 [b, d_out] alone, that stay valid
+ * until the next callback for this trainer), and for blocks
  * with ADLOCO_GRAD_PROVIDED maintains grad_sum itself: it STORES its gradient sum there when
  * micro_step is 0 (the driver does not clear such blocks between inner steps) and adds to it when
  * micro_step > 0.  Device work of the callback

@@ -182,9 +182,10 @@ template <typename E, bool FAST> __global__ __launch_bounds__(kPackThreads) void
 // have to be under way all the time: the workgroup meets twice per block and refills in two parts whatever has been read --
 // after the first half of A's blocks their place and B's, after the second half theirs -- which gives every load one and a
 // half blocks of time until it is needed, out of two stages.
-//   Measured: 32768 x 5632 x 2048 to bf16 291 us, 2.6 PFLOP/s; 8192^3 375 us, 2.9; 16384^3 2.69 ms, 3.3.  fp32 out: 8192^3 815 us,
-// 1.35 PFLOP/s; 1024 x 4096 x 32033 228 us, 1.2.  The matrix cores are busy for 73 % and 56 % of the cycles (and the clock falls
-// to 1.7 and 1.9 GHz under them); in the second, widening takes as many vector cycles as the products take matrix cycles.
+//   Measured, these and the figures further down on one card in one go (cards differ by 5 %, and so does one with what it ran
+// just before): 32768 x 5632 x 2048 to bf16 281 to 292 us, 2.6 PFLOP/s; 8192^3 344 us, 3.2; 16384^3 2.68 ms, 3.3.  fp32 out: 8192^3
+// 801 us, 1.37 PFLOP/s; 1024 x 4096 x 32033 214 us, 1.26.  The matrix cores are busy for 73 % and 56 % of the cycles (and the clock
+// falls to 1.7 and 1.9 GHz under them); in the second, widening takes as many vector cycles as the products take matrix cycles.
 // ---------------------------------------------------------------------------------------------------------------------
 typedef __attribute__((ext_vector_type(8))) int mfma_i32x8;
 typedef __attribute__((ext_vector_type(4))) int i32x4;
@@ -653,8 +654,8 @@ template <int EDGE_M, int EDGE_N, typename E> __global__ __launch_bounds__(256) 
 // ---------------------------------------------------------------------------------------------------------------------
 // Few rows of A (up to 32): B is read once, by whoever multiplies it, straight into registers; all else is latency.  A
 // workgroup takes 16 columns, its waves share the blocks of k among them and add up what they have through LDS, in order.
-// 3 x 5632 x 2048: 5.2 us (on small tiles 11), 2.2 TB/s of B; 33 to 64 rows would take 13 us, on small tiles 10.  Widened like
-// fp32 outputs whatever the output is: the vector and matrix cores wait for memory anyway (8-bit instruction / widened:
+// 3 x 5632 x 2048: 5.4 us, 2.1 TB/s of B (with the host's part 8.0, on small tiles 9.2); 33 to 64 rows would take 13 us, on
+// small tiles 10.  Widened like fp32 outputs whatever the output is: the vector and matrix cores wait for memory anyway (8-bit instruction / widened:
 // 3 x 5632 x 2048 7.0 / 7.0 us with the host, 32 x 8192 x 8192 24.9 / 25.3, 8 x 4096 x 14336 15.0 / 15.4).
 // ---------------------------------------------------------------------------------------------------------------------
 constexpr int kFewRows = 32;
@@ -757,7 +758,7 @@ template <typename E> hipError_t launch_few(const ProductArgs& p, hipStream_t st
   return p.M <= 16 ? launch_few_rows<1, E>(p, st) : launch_few_rows<2, E>(p, st);
 }
 // More large tiles than compute units, whole, of an even number of blocks: one workgroup per compute unit walks over them (one
-// workgroup per tile / walking: 32768 x 5632 x 2048 357 / 342 us, x 512 118 / 114, 8192 x 8192 x 1024 66 / 64).
+// workgroup per tile / walking: 32768 x 5632 x 2048 300 / 292 us, x 512 120 / 115, 8192 x 8192 x 1024 68.6 / 66.0).
 template <typename E> hipError_t launch_product(const ProductArgs& p, bool large, bool exact, hipStream_t st) {
   if constexpr (!std::is_same<E, float>::value) {
     if (large) {
@@ -773,9 +774,10 @@ template <typename E> hipError_t launch_product(const ProductArgs& p, bool large
 // shapes (1 to 32768 rows, 64 to 8192 columns, 128 to 32768 values of k; log error 13 %): 0.36 a block of k for a small tile
 // that has its compute unit to itself and 0.95 for two that share it (exact products 0.75 and 1.5), 0.93 for a large tile, 3.0
 // and 6.5 to start and store one; 1.7 and the partial tiles' way out and back for a second kernel.  The choice is within 4 %
-// of the best one on average.  Measured, few rows / small tiles / small tiles in 4 pieces / large: 3 x 5632 x 2048 7 / 11 / 11
-// / 23, 64 x 8192 x 8192 - / 29 / 20 / 60, 512 x 5632 x 2048 - / 15 / 26 / 35, 32768 x 5632 x 2048 - / 376 / - / 300 us.
-// Rows of the output that are not 16-byte aligned count 12 us more for a large tile (32001 x 2044 x 1024: small 78, large 104).
+// of the best one on average.  Measured with the host's 7 us, few rows / small tiles / small tiles in 4 pieces / large:
+// 3 x 5632 x 2048 8.0 / 9.2 / 10.7 / 20, 64 x 8192 x 8192 - / 28 / 20 / 64, 512 x 5632 x 2048 - / 11 / 25 / 21, 32768 x 5632 x 2048
+// - / 364 / - / 281 us.  Rows of the output that are not 16-byte aligned count 12 us more for a large tile (32001 x 2044 x 1024:
+// small 79, large 97).
 struct ProductChoice { int kernel, pieces; };          // kernel: 1 few rows, 4 small tiles, 8 large ones
 ProductChoice choose_product(long long M, long long N, int steps, bool exact, bool aligned, int kernel, int pieces, bool split) {
   ProductChoice best{4, 1};
