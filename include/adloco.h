@@ -527,10 +527,10 @@ int adloco_pack_blocks(adloco_ctx* ctx, const void* x, int64_t x_row_stride, int
  * faster kernel).  For other 16-bit outputs the 8-bit instruction cuts each off below 2^-13 of the largest of its
  * group: 1.5e-5 of a sum of Gaussian values, a tenth of fp16's own rounding, but products that cancel leave that
  * much of their own size.  ADLOCO_EXACT_PRODUCTS makes those exact as well, in about twice the time.
- * Exact products take their operands as bf16: what lies below 2^-133 (blocks of exponents
- * 0 to 2) is rounded to a multiple of it, and 2^128 and more (values above 3.29e38 before they were packed) is
- * infinite.  A NaN in row m of a makes row m of out NaN, one in row n of b column n; the exponent 255 is a block of
- * NaN.  Rows are at most 2^23 bytes apart, and out has at most 2^24 - 8 tiles of 128 x 128. */
+ * Exact products take their operands as bf16: what lies below 2^-133 (blocks of exponents 0 to 2) is rounded to a
+ * multiple of it, and 2^128 and more (values above 3.29e38 before they were packed) is infinite.  A NaN in row m of a
+ * makes row m of out NaN, one in row n of b column n; the exponent 255 is a block of NaN.  Rows are at most 2^23 bytes
+ * apart, and out has at most 2^24 - 8 tiles of 128 x 128. */
 int adloco_block_product(adloco_ctx* ctx, const adloco_blocks8* a, const adloco_blocks8* b, void* out,
                          int64_t out_row_stride, int dtype, uint32_t flags, void* stream);
 
@@ -559,8 +559,8 @@ int adloco_rms_norm(adloco_ctx* ctx, const adloco_norm_io* io, int64_t rows, int
  *   gain_sums[i] = sum over the T rows of sample i of dy n
  *   h, dy, dh, dx  [B * T, d]; dh and dx may each be h, dy or dh_in; at least one of dh, dx, gain_sums
  *   dh_in          [B * T, d] or NULL: the gradient that reaches h on the residual path
- *   gain_sums      device [B, d] fp32 or NULL; sums of a sample run in a fixed order, long ones in pieces (T rows in one piece
- *                  are off by about 2 sqrt(T) roundings at most, 256 at least)
+ *   gain_sums      device [B, d] fp32 or NULL; sums of a sample run in a fixed order and in pieces: T rows are off by
+ *                  about 2 sqrt(T) roundings at most, short samples by T
  * d <= 16384, B * T < 2^31. */
 typedef struct {
   const void*  h;

@@ -655,8 +655,9 @@ template <int EDGE_M, int EDGE_N, typename E> __global__ __launch_bounds__(256) 
 // Few rows of A (up to 32): B is read once, by whoever multiplies it, straight into registers; all else is latency.  A
 // workgroup takes 16 columns, its waves share the blocks of k among them and add up what they have through LDS, in order.
 // 3 x 5632 x 2048: 5.4 us, 2.1 TB/s of B (with the host's part 8.0, on small tiles 9.2); 33 to 64 rows would take 13 us, on
-// small tiles 10.  Widened like fp32 outputs whatever the output is: the vector and matrix cores wait for memory anyway (8-bit instruction / widened:
-// 3 x 5632 x 2048 7.0 / 7.0 us with the host, 32 x 8192 x 8192 24.9 / 25.3, 8 x 4096 x 14336 15.0 / 15.4).
+// small tiles 10.  Widened like fp32 outputs whatever the output is: the vector and matrix cores wait for memory anyway (8-bit
+// instruction / widened, with the host's part: 3 x 5632 x 2048 7.0 / 7.0 us, 32 x 8192 x 8192 24.9 / 25.3, 8 x 4096 x 14336
+// 15.0 / 15.4).
 // ---------------------------------------------------------------------------------------------------------------------
 constexpr int kFewRows = 32;
 
